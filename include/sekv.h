@@ -71,7 +71,7 @@ typedef enum {
     SEKV_ERR_HIP = 4            /* a HIP runtime call failed; see sekv_last_error()  */
 } sekv_status;
 
-typedef enum { SEKV_F32 = 0, SEKV_BF16 = 1 } sekv_dtype;
+typedef enum { SEKV_F32 = 0, SEKV_BF16 = 1, SEKV_E4M3 = 2 /* page storage only */ } sekv_dtype;
 
 /* Implementation choice for the zoomed spans (sekv_dims.flags bits 0..1). */
 #define SEKV_ZOOM_DEFAULT 0     /* library default (currently FACTORED)                     */
@@ -159,7 +159,8 @@ SEKV_API sekv_status sekv_workspace_init(void *ws, size_t ws_bytes, hipStream_t 
 /* Read and clear the workspace's device error word (synchronises `stream`).  Bits:
  * 1 = a wait for a selection timed out, 2 = a factor block lay outside the arena or its
  * rank-table entry was invalid, 4 = a selected index was out of range (sekv_build_cache:
- * an anchor index or span outside the sequence's tokens).  0 after every correct call. */
+ * an anchor index or span outside the sequence's tokens), 8 = a page lay outside the pool or
+ * a token outside its sequence's pages (sekv_page_*).  0 after every correct call. */
 SEKV_API sekv_status sekv_workspace_status(void *ws, size_t ws_bytes, hipStream_t stream,
                                   int32_t *error_bits);
 
@@ -325,6 +326,98 @@ SEKV_API sekv_status sekv_build_cache(const sekv_build_dims *dims, const void *k
                                       double *span_logsize, void *factors, int64_t factors_bytes,
                                       const int64_t *block_off, void *ws, size_t ws_bytes,
                                       hipStream_t stream);
+
+/* ----------------------------------------------------------------------------------
+ * Paged token store, and attention over it: the time before a layer has its span cache.
+ * A prompt arrives in chunks (a decode step is a chunk of one token).  Per chunk,
+ * sekv_page_append stores the new tokens' keys and values and sekv_page_attend lets their
+ * queries attend to everything stored so far; at the end sekv_page_read hands the rows to
+ * the builder above as [B][Hkv][N][d].
+ *
+ * Pages are rows of a pool [n_pages][Hkv][page_size][d] for keys and one for values; token t
+ * of sequence b is row t % page_size of page table[b][t / page_size].  Rows are held in
+ * dims.dtype, or (page_dtype = SEKV_E4M3) as one byte a value and one exponent byte a row:
+ *   value = code * 2^(E - 127), code an e4m3 number (sign, 4 bits of exponent, 3 of mantissa,
+ *   largest 448, no infinity), E the smallest exponent with max |x| <= 448 * 2^(E - 127) over
+ *   the row's finite values, at least 1; E = 127 for a row without finite non-zero values.
+ * The scale is a power of two, so scaling is exact and a stored value is off by at most half
+ * an e4m3 step (2^-4 of it, or 2^-10 * 2^(E - 127) for the smallest); read back in dims.dtype
+ * it is exact again.  Infinities and NaN are stored as NaN in 8 bits.
+ *
+ * Ragged batches: the new tokens of all sequences lie one after another; sequence b has rows
+ * tok_start[b] .. tok_start[b + 1] - 1 of n_tokens (tok_start int32 [B + 1], ascending from 0;
+ * rows at tok_start[B] and behind are neither read nor written).  seq_len[b] counts the
+ * sequence's tokens with the new ones, so new token i of n_new stands at position
+ * seq_len[b] - n_new + i.  Both tables are read on the device: a captured graph may be
+ * replayed with other contents.
+ *
+ * Bad tables give a wrong answer and error bit 8, never an access outside the buffers: a page
+ * outside [0, n_pages) takes no part (not written, not read, its keys not seen), nor does a
+ * token at a position below 0 (for sekv_page_append) or at max_pages * page_size and behind.
+ * Entries of the table behind a sequence's last token are not read.  Two rows of one
+ * sekv_page_append that fall into the same slot race: share pages between sequences only
+ * where none of their rows is written.
+ * -------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t batch;          /* 0 <= B <= 4096                                              */
+    int32_t n_q_heads;      /* Hq; query head h reads KV head h / (Hq / Hkv)               */
+    int32_t n_kv_heads;     /* Hkv; Hq / Hkv in {1, 2, 4, 8}                               */
+    int32_t head_dim;       /* d in {64, 128}                                              */
+    int32_t page_size;      /* tokens a page: a power of two, 1..1024                      */
+    int32_t n_pages;        /* pages in the pool, n_pages * Hkv * page_size < 2^31         */
+    int32_t max_pages;      /* row stride of the page table, max_pages * page_size <= 2^30 */
+    int32_t dtype;          /* SEKV_F32 or SEKV_BF16: new tokens, queries, outputs          */
+    int32_t page_dtype;     /* dtype, or SEKV_E4M3                                         */
+    int32_t window;         /* a query sees at most this many keys, its own last; 0: all   */
+    int32_t reserved[2];    /* 0                                                           */
+    double softmax_scale;
+} sekv_page_dims;
+
+/* One layer's pages.  Device pointers, caller-owned; pools 16-byte aligned. */
+typedef struct {
+    void *k;                /* [n_pages][Hkv][page_size][d] in page_dtype                  */
+    void *v;
+    uint8_t *k_scale;       /* [n_pages][Hkv][page_size] exponents E; NULL unless E4M3     */
+    uint8_t *v_scale;
+    const int32_t *table;   /* [B][max_pages]                                              */
+    const int32_t *seq_len; /* [B]                                                         */
+} sekv_pages;
+
+/* Validate dims without launching anything. */
+SEKV_API sekv_status sekv_check_page_dims(const sekv_page_dims *dims);
+
+/* Bytes of device workspace the calls below need for up to n_tokens new tokens (0 if dims are
+ * invalid).  Initialise it once with sekv_workspace_init; its error word is read with
+ * sekv_workspace_status.  sekv_page_append and sekv_page_read use the error word only (256
+ * bytes are enough for them). */
+SEKV_API size_t sekv_page_workspace_size(const sekv_page_dims *dims, int32_t n_tokens);
+
+/* Store the new tokens: k, v [n_tokens][Hkv][d] in dims.dtype, consecutive tokens k_stride and
+ * v_stride elements apart (at least Hkv * d; 16-byte multiples), as slices of a projection's
+ * output are. */
+SEKV_API sekv_status sekv_page_append(const sekv_page_dims *dims, const sekv_pages *pages, const void *k,
+                                      const void *v, int64_t k_stride, int64_t v_stride,
+                                      const int32_t *tok_start, int32_t n_tokens, void *ws, size_t ws_bytes,
+                                      hipStream_t stream);
+
+/* Read rows 0 .. min(seq_len[b], max_tokens) - 1 of every sequence into keys and values
+ * [B][Hkv][max_tokens][d] in dims.dtype (the layout of sekv_build_cache); rows behind, and
+ * rows whose page is outside the pool, are left as they are. */
+SEKV_API sekv_status sekv_page_read(const sekv_page_dims *dims, const sekv_pages *pages, void *keys,
+                                    void *values, int32_t max_tokens, void *ws, size_t ws_bytes,
+                                    hipStream_t stream);
+
+/* Causal attention of the new tokens: q [n_tokens][Hq][d], tokens q_stride elements apart; a
+ * query at position p sees the keys max(0, p - window + 1) .. p of its sequence (their rows
+ * have to be stored before, in stream order).  Writes out [n_tokens][Hq][d] in dims.dtype and,
+ * unless NULL, lse float [n_tokens][Hq], the natural logarithm of the softmax's denominator.
+ * A query that sees nothing (position below 0) gets zeros and -inf.  Keys and values that a
+ * query does not see do not reach it, whatever they hold.
+ * Scores and sums are held in float; with bfloat16 tokens the softmax weights are rounded to
+ * bfloat16 for the matrix cores (off by at most 2^-8 of each); with float tokens nothing is. */
+SEKV_API sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages, const void *q,
+                                      int64_t q_stride, const int32_t *tok_start, int32_t n_tokens,
+                                      void *out, float *lse, void *ws, size_t ws_bytes, hipStream_t stream);
 
 /* ----------------------------------------------------------------------------------
  * Several layers in one HIP graph.  A decode step of an L-layer model runs the step

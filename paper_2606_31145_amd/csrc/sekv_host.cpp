@@ -1,6 +1,8 @@
 // Host-only logic of the library (see sekv_host.h).  No HIP runtime calls.
 #include "sekv_host.h"
 
+#include "sekv_page_internal.h"
+
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>
@@ -297,6 +299,57 @@ bool WsTracker::before_launch(uintptr_t ws, size_t bytes, uint64_t key, uint64_t
     return zero;
 }
 
+// ---- paged token store ----------------------------------------------------------------
+
+sekv_status check_page_dims(const sekv_page_dims *d) {
+    if (!d) return fail(SEKV_ERR_INVALID_ARG, "page dims is NULL");
+    if (d->batch < 0) return fail(SEKV_ERR_INVALID_ARG, "batch < 0");
+    if (d->batch > kMaxPageBatch) return fail(SEKV_ERR_UNSUPPORTED, "batch %d > %d", d->batch, kMaxPageBatch);
+    if (d->n_q_heads <= 0 || d->n_kv_heads <= 0)
+        return fail(SEKV_ERR_INVALID_ARG, "head counts must be positive");
+    if (d->n_q_heads % d->n_kv_heads)
+        return fail(SEKV_ERR_INVALID_ARG, "n_q_heads %% n_kv_heads != 0");
+    const int G = d->n_q_heads / d->n_kv_heads;
+    if (G != 1 && G != 2 && G != 4 && G != 8)
+        return fail(SEKV_ERR_UNSUPPORTED, "group size %d not in {1,2,4,8}", G);
+    if (d->n_q_heads > 4096) return fail(SEKV_ERR_UNSUPPORTED, "n_q_heads %d > 4096", d->n_q_heads);
+    if (d->head_dim != 64 && d->head_dim != 128)
+        return fail(SEKV_ERR_UNSUPPORTED, "head_dim %d not in {64,128}", d->head_dim);
+    if (d->page_size < 1 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)))
+        return fail(SEKV_ERR_UNSUPPORTED, "page_size %d: a power of two in [1, 1024]", d->page_size);
+    if (d->n_pages < 1 || d->max_pages < 1)
+        return fail(SEKV_ERR_INVALID_ARG, "n_pages/max_pages < 1");
+    if ((long long)d->n_pages * d->n_kv_heads * d->page_size > 0x7fffffffll)
+        return fail(SEKV_ERR_UNSUPPORTED, "pool of %d pages too large", d->n_pages);
+    if ((long long)d->max_pages * d->page_size > (1ll << 30))
+        return fail(SEKV_ERR_UNSUPPORTED, "max_pages %d too large", d->max_pages);
+    if (d->dtype != SEKV_F32 && d->dtype != SEKV_BF16)
+        return fail(SEKV_ERR_UNSUPPORTED, "dtype %d", d->dtype);
+    if (d->page_dtype != d->dtype && d->page_dtype != SEKV_E4M3)
+        return fail(SEKV_ERR_UNSUPPORTED, "page_dtype %d with dtype %d", d->page_dtype, d->dtype);
+    if (d->window < 0) return fail(SEKV_ERR_INVALID_ARG, "window < 0");
+    if (d->reserved[0] != 0 || d->reserved[1] != 0)
+        return fail(SEKV_ERR_INVALID_ARG, "reserved field is not 0");
+    if (!(d->softmax_scale > 0.0) || !std::isfinite(d->softmax_scale))
+        return fail(SEKV_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    return SEKV_OK;
+}
+
+sekv_status check_pages(const sekv_page_dims *d, const sekv_pages *p) {
+    if (!p) return fail(SEKV_ERR_INVALID_ARG, "pages is NULL");
+    if (!p->k || !p->v || !p->table || !p->seq_len)
+        return fail(SEKV_ERR_INVALID_ARG, "pages.k, v, table or seq_len is NULL");
+    if (misaligned(p->k, 16) || misaligned(p->v, 16))
+        return fail(SEKV_ERR_INVALID_ARG, "page pools not 16-byte aligned");
+    if (misaligned(p->table, 4) || misaligned(p->seq_len, 4))
+        return fail(SEKV_ERR_INVALID_ARG, "page table or seq_len not 4-byte aligned");
+    const bool e4m3 = d->page_dtype == SEKV_E4M3;
+    if (e4m3 && (!p->k_scale || !p->v_scale))
+        return fail(SEKV_ERR_INVALID_ARG, "pages.k_scale or v_scale is NULL");
+    if (!e4m3 && (p->k_scale || p->v_scale))
+        return fail(SEKV_ERR_INVALID_ARG, "scales given for pages without them");
+    return SEKV_OK;
+}
 
 // ---- prefill-side builder: dims check and the factor arena's layout -----------------
 

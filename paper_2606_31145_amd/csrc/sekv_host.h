@@ -86,6 +86,11 @@ class WsTracker {
     uint64_t clock_ = 0;
 };
 
+// ---- paged token store ----------------------------------------------------------------
+sekv_status check_page_dims(const sekv_page_dims *d);
+// Pointer checks of a page store (null, alignment, scales present just when they are used).
+sekv_status check_pages(const sekv_page_dims *d, const sekv_pages *p);
+
 // ---- prefill-side builder ------------------------------------------------------------
 sekv_status check_build_dims(const sekv_build_dims *d);
 // The factor arena of a segmentation from host copies of n_spans [B] and span_len

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_PKG, "libsekv_trace.so" if os.environ.get("SEKV_LIB") =
                         else "libsekv.so")
 
 SEKV_OK, SEKV_ERR_INVALID_ARG, SEKV_ERR_UNSUPPORTED, SEKV_ERR_WORKSPACE, SEKV_ERR_HIP = range(5)
-SEKV_F32, SEKV_BF16 = 0, 1
+SEKV_F32, SEKV_BF16, SEKV_E4M3 = 0, 1, 2
 SEKV_ZOOM_DEFAULT, SEKV_ZOOM_FACTORED = 0, 1
 SEKV_TIER_GATHER, SEKV_TIER_MEMCPY = 0, 1
 TIER_MODES = {"gather": SEKV_TIER_GATHER, "memcpy": SEKV_TIER_MEMCPY}
@@ -34,7 +34,8 @@ EXPORTED = ("sekv_status_string", "sekv_last_error", "sekv_phase_trace", "sekv_c
             "sekv_validate_cache", "sekv_decode_step_noalloc", "sekv_route_gated",
             "sekv_decode_step_gated", "sekv_segment_workspace_size", "sekv_segment",
             "sekv_build_layout", "sekv_build_cache", "sekv_decode_layers_tiered",
-            "sekv_tier_layer_stats")
+            "sekv_tier_layer_stats", "sekv_check_page_dims", "sekv_page_workspace_size",
+            "sekv_page_append", "sekv_page_read", "sekv_page_attend")
 
 
 class SekvError(RuntimeError):
@@ -83,6 +84,21 @@ class BuildDims(ctypes.Structure):
                 ("sweeps", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("power", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("alpha", ctypes.c_double)]
+
+
+class PageDims(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("page_dtype", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("reserved", ctypes.c_int32 * 2), ("softmax_scale", ctypes.c_double)]
+
+
+class PagesStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("seq_len", ctypes.c_void_p)]
 
 
 def _load():
@@ -151,6 +167,18 @@ def _load():
     lib.sekv_build_cache.argtypes = [P(BuildDims), VP, VP, VP, VP, VP, VP, VP, VP, VP, VP,
                                      ctypes.c_int32, ctypes.c_int32, VP, VP, VP, VP, VP, VP, VP,
                                      ctypes.c_int64, VP, VP, SZ, VP]
+    lib.sekv_check_page_dims.restype = ctypes.c_int
+    lib.sekv_check_page_dims.argtypes = [P(PageDims)]
+    lib.sekv_page_workspace_size.restype = SZ
+    lib.sekv_page_workspace_size.argtypes = [P(PageDims), ctypes.c_int32]
+    lib.sekv_page_append.restype = ctypes.c_int
+    lib.sekv_page_append.argtypes = [P(PageDims), P(PagesStruct), VP, VP, ctypes.c_int64, ctypes.c_int64, VP,
+                                     ctypes.c_int32, VP, SZ, VP]
+    lib.sekv_page_read.restype = ctypes.c_int
+    lib.sekv_page_read.argtypes = [P(PageDims), P(PagesStruct), VP, VP, ctypes.c_int32, VP, SZ, VP]
+    lib.sekv_page_attend.restype = ctypes.c_int
+    lib.sekv_page_attend.argtypes = [P(PageDims), P(PagesStruct), VP, ctypes.c_int64, VP, ctypes.c_int32, VP, VP,
+                                     VP, SZ, VP]
     return lib
 
 
@@ -666,3 +694,169 @@ def build_layer(bd: BuildDims, keys, values, surprisal, n_tokens, omega, ws: Wor
               "max_span_len": max([int(span_len[b, :ns[b]].max(initial=1)) for b in range(bd.batch)],
                                   default=1)}
     return cache, seg, layout
+
+
+# ---------------------------------------------------------------------------
+# paged token store
+# ---------------------------------------------------------------------------
+
+def make_page_dims(*, batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, dtype,
+                   page_dtype=None, window=0, softmax_scale) -> PageDims:
+    """dtype "f32" or "bf16"; page_dtype the same (default) or "e4m3"."""
+    dt = DTYPE_CODES[dtype] if isinstance(dtype, str) else int(dtype)
+    pt = dt if page_dtype is None else SEKV_E4M3 if page_dtype == "e4m3" else \
+        DTYPE_CODES[page_dtype] if isinstance(page_dtype, str) else int(page_dtype)
+    return PageDims(batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, dt, pt, int(window),
+                    (ctypes.c_int32 * 2)(0, 0), float(softmax_scale))
+
+
+def check_page_dims(pd: PageDims):
+    _check(LIB.sekv_check_page_dims(ctypes.byref(pd)))
+
+
+def page_workspace_size(pd: PageDims, new_tokens: int) -> int:
+    """Bytes for Workspace(None, device, nbytes=...) that serves up to new_tokens new tokens."""
+    n = int(LIB.sekv_page_workspace_size(ctypes.byref(pd), int(new_tokens)))
+    if n == 0:
+        raise SekvError(SEKV_ERR_INVALID_ARG, LIB.sekv_last_error().decode())
+    return n
+
+
+_PAGE_STORAGE = {SEKV_F32: torch.float32, SEKV_BF16: torch.bfloat16, SEKV_E4M3: torch.float8_e4m3fn}
+
+
+class PageCache:
+    """Device tensors of one layer's pages, laid out as sekv_pages describes: pools
+    [n_pages][Hkv][page_size][d] (float8_e4m3fn with uint8 exponents [n_pages][Hkv][page_size],
+    or the tokens' own type without), page table int32 [B][max_pages], seq_len int32 [B]."""
+
+    def __init__(self, k_pages, v_pages, page_table, seq_len, k_scale=None, v_scale=None):
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.page_table, self.seq_len = page_table, seq_len
+
+    @classmethod
+    def empty(cls, pd: PageDims, page_table, seq_len, device="cuda"):
+        """Pools of zeros for pd."""
+        check_page_dims(pd)
+        shape = (pd.n_pages, pd.n_kv_heads, pd.page_size, pd.head_dim)
+        k, v = (torch.zeros(shape, dtype=_PAGE_STORAGE[pd.page_dtype], device=device) for _ in "kv")
+        if pd.page_dtype != SEKV_E4M3:
+            return cls(k, v, page_table, seq_len)
+        ks, vs = (torch.full(shape[:-1], 127, dtype=torch.uint8, device=device) for _ in "kv")
+        return cls(k, v, page_table, seq_len, ks, vs)
+
+    def struct(self, pd: PageDims) -> PagesStruct:
+        """Checked against pd: types, sizes, one device."""
+        rows = (pd.n_pages, pd.n_kv_heads, pd.page_size)
+        want = _PAGE_STORAGE[pd.page_dtype] if pd.page_dtype in _PAGE_STORAGE else None
+        dev = self.k_pages.device
+        for name, x, dt, shape in (("k_pages", self.k_pages, want, rows + (pd.head_dim,)),
+                                   ("v_pages", self.v_pages, want, rows + (pd.head_dim,)),
+                                   ("k_scale", self.k_scale, torch.uint8, rows),
+                                   ("v_scale", self.v_scale, torch.uint8, rows),
+                                   ("page_table", self.page_table, torch.int32, (pd.batch, pd.max_pages)),
+                                   ("seq_len", self.seq_len, torch.int32, (pd.batch,))):
+            if x is None and dt is torch.uint8:
+                continue
+            _expect(x, name, dt, shape, dev)
+        return PagesStruct(_ptr(self.k_pages), _ptr(self.v_pages), _ptr(self.k_scale), _ptr(self.v_scale),
+                           _ptr(self.page_table), _ptr(self.seq_len))
+
+
+def _expect(x, name, dtype, shape, device):
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if x.dtype != dtype or tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, expected {dtype} {tuple(shape)}")
+    if x.device != device:
+        raise ValueError(f"{name} is on {x.device}, the pages on {device}")
+
+
+def _token_rows(pd: PageDims, x, name, heads, n_tokens, device):
+    """The token stride of [n_tokens][heads][d] rows that are contiguous within a token."""
+    _expect(x, name, _PAGE_STORAGE[pd.dtype], (n_tokens, heads, pd.head_dim), device)
+    d = pd.head_dim
+    if n_tokens == 0:
+        return heads * d
+    if x.stride(2) != 1 or (heads > 1 and x.stride(1) != d):
+        raise ValueError(f"{name}: a token's heads have to lie one after another")
+    return x.stride(0) if n_tokens > 1 else heads * d
+
+
+def _tok_start(pd: PageDims, tok_start, device):
+    _expect(tok_start, "tok_start", torch.int32, (pd.batch + 1,), device)
+    return _ptr(tok_start)
+
+
+def _on(device, stream):
+    """The device and stream context of a call: the caller's stream, else the device's current one."""
+    if device.type != "cuda":
+        raise ValueError("the pages have to be on a GPU")
+    if stream is None:
+        return torch.cuda.device(device), torch.cuda.current_stream(device).cuda_stream
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return torch.cuda.stream(stream), stream.cuda_stream
+
+
+def page_append(pd: PageDims, cache: PageCache, k, v, tok_start, ws: Workspace, stream=None):
+    """sekv_page_append: stores k, v [n_tokens][Hkv][d] (tokens may be strided) in the pages."""
+    cs, dev = cache.struct(pd), cache.k_pages.device
+    n = k.shape[0]
+    sk = _token_rows(pd, k, "k", pd.n_kv_heads, n, dev)
+    sv = _token_rows(pd, v, "v", pd.n_kv_heads, n, dev)
+    ts = _tok_start(pd, tok_start, dev)
+    ctx, st = _on(dev, stream)
+    with ctx:
+        _check(LIB.sekv_page_append(ctypes.byref(pd), ctypes.byref(cs), k.data_ptr(), v.data_ptr(), sk, sv, ts, n,
+                                    ws.ptr, ws.nbytes, st))
+
+
+def page_read(pd: PageDims, cache: PageCache, max_tokens: int, ws: Workspace, keys=None, values=None, stream=None):
+    """sekv_page_read: (keys, values) [B][Hkv][max_tokens][d]; rows behind a sequence's last token
+    are left as given, zeros in tensors allocated here."""
+    cs, dev = cache.struct(pd), cache.k_pages.device
+    shape = (pd.batch, pd.n_kv_heads, int(max_tokens), pd.head_dim)
+    ctx, st = _on(dev, stream)
+    with ctx:
+        if keys is None:
+            keys = torch.zeros(shape, dtype=_PAGE_STORAGE[pd.dtype], device=dev)
+        if values is None:
+            values = torch.zeros(shape, dtype=_PAGE_STORAGE[pd.dtype], device=dev)
+        _expect(keys, "keys", _PAGE_STORAGE[pd.dtype], shape, dev)
+        _expect(values, "values", _PAGE_STORAGE[pd.dtype], shape, dev)
+        _check(LIB.sekv_page_read(ctypes.byref(pd), ctypes.byref(cs), _ptr(keys), _ptr(values), int(max_tokens),
+                                  ws.ptr, ws.nbytes, st))
+    return keys, values
+
+
+def page_attend(pd: PageDims, cache: PageCache, q, tok_start, ws: Workspace, out=None, lse=None,
+                want_lse: bool = False, stream=None):
+    """sekv_page_attend: (out [n_tokens][Hq][d], lse float [n_tokens][Hq] or None) of the queries
+    q [n_tokens][Hq][d] (tokens may be strided)."""
+    cs, dev = cache.struct(pd), cache.k_pages.device
+    n = q.shape[0]
+    sq = _token_rows(pd, q, "q", pd.n_q_heads, n, dev)
+    ts = _tok_start(pd, tok_start, dev)
+    ctx, st = _on(dev, stream)
+    with ctx:
+        if out is None:
+            out = torch.empty((n, pd.n_q_heads, pd.head_dim), dtype=q.dtype, device=dev)
+        if lse is None and want_lse:
+            lse = torch.empty((n, pd.n_q_heads), dtype=torch.float32, device=dev)
+        _expect(out, "out", q.dtype, (n, pd.n_q_heads, pd.head_dim), dev)
+        if lse is not None:
+            _expect(lse, "lse", torch.float32, (n, pd.n_q_heads), dev)
+        _check(LIB.sekv_page_attend(ctypes.byref(pd), ctypes.byref(cs), q.data_ptr(), sq, ts, n, _ptr(out), _ptr(lse),
+                                    ws.ptr, ws.nbytes, st))
+    return out, lse
+
+
+def build_layer_paged(bd: BuildDims, pd: PageDims, cache: PageCache, surprisal, omega, ws: Workspace, stream=None):
+    """build_layer on the rows of a paged store: every sequence's stored tokens (cache.seq_len) are
+    read back and become the layer's span cache."""
+    if (bd.batch, bd.n_kv_heads, bd.head_dim, bd.dtype) != (pd.batch, pd.n_kv_heads, pd.head_dim, pd.dtype):
+        raise ValueError("build and page dims differ in batch, KV heads, head_dim or dtype")
+    keys, values = page_read(pd, cache, bd.max_tokens, ws, stream=stream)
+    return build_layer(bd, keys, values, surprisal, cache.seq_len, omega, ws, stream)

@@ -1,0 +1,309 @@
+"""Paged token store on the GPU against the plain form in 64 bits: what is stored and read back bit
+for bit, attention within the bound that its roundings allow (Case.attend)."""
+
+import math
+import zlib
+
+import pytest
+import torch
+
+from tests.gpu_common import banner
+from tests.page_common import TORCH, Case, encode_rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2606_31145_amd import sekv
+    return sekv
+
+
+def _seed(*a):
+    return zlib.crc32(repr(a).encode())
+
+
+STORES = [("bf16", "same"), ("bf16", "e4m3"), ("f32", "same"), ("f32", "e4m3")]
+
+
+def _expected_pools(c):
+    """Pools after the append: codes and exponents (or rows) at the new tokens' places."""
+    want = {n: [c.codes[n][0].clone(), None if c.codes[n][1] is None else c.codes[n][1].clone()] for n in "kv"}
+    for b, (n, nq) in enumerate(zip(c.lens, c.news)):
+        for i in range(nq):
+            p = n - nq + i
+            if p < 0:
+                continue
+            page, slot = int(c.table[b, p // c.page]), p % c.page
+            if not 0 <= page < c.n_pages:
+                continue
+            for name, src in (("k", c.k), ("v", c.v)):
+                x = src[c.start[b] + i]
+                if c.store == "e4m3":
+                    want[name][0][page, :, slot], want[name][1][page, :, slot] = encode_rows(x)
+                else:
+                    want[name][0][page, :, slot] = x
+    return want
+
+
+def _same(got, want):
+    """Equal bits; in 8 bits any NaN is as good as another."""
+    got = got.cpu()
+    if got.dtype == torch.float8_e4m3fn:
+        g, w = got.view(torch.uint8), want
+        return torch.equal(torch.where(g & 127 == 127, 127, g), torch.where(w & 127 == 127, 127, w))
+    if got.is_floating_point():
+        i = torch.int16 if got.dtype == torch.bfloat16 else torch.int32
+        return torch.equal(got.view(i), want.view(i))
+    return torch.equal(got, want)
+
+
+def _check_append(S, c, bits=0):
+    cache, ws = c.cache(S), c.workspace(S)
+    S.page_append(c.dims(S), cache, c.k.to("cuda") if c.k.is_contiguous() else _strided(c, "k"),
+                  c.v.to("cuda") if c.v.is_contiguous() else _strided(c, "v"), c.tok_start(), ws)
+    torch.cuda.synchronize()
+    want = _expected_pools(c)
+    for name, pool, scale in (("k", cache.k_pages, cache.k_scale), ("v", cache.v_pages, cache.v_scale)):
+        assert _same(pool, want[name][0]), name
+        if scale is not None:
+            assert _same(scale, want[name][1]), name
+    assert ws.status() == bits
+
+
+def _strided(c, name):
+    """The same strided view of one device tensor."""
+    x = getattr(c, name)
+    base = torch.as_strided(x, (x.shape[0], x.stride(0) // c.d, c.d), (x.stride(0), c.d, 1), 0).to("cuda")
+    at = x.storage_offset() // c.d
+    return base[:, at:at + x.shape[1]]
+
+
+APPENDS = [
+    dict(lens=[1], news=[1]),
+    dict(lens=[40, 7, 0, 33], news=[1, 1, 0, 1], page=16),
+    dict(lens=[17, 300, 64], news=[17, 123, 0], page=32, kv_heads=3, group=1),
+    dict(lens=[5, 1000], news=[5, 777], page=128, dim=128, kv_heads=1, group=8, strided=True),
+    dict(lens=[9, 31], news=[4, 31], page=1, dim=128),
+    dict(lens=[2100], news=[2050], page=1024, kv_heads=2, strided=True, tail=5),
+]
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+@pytest.mark.parametrize("kw", APPENDS, ids=lambda k: "-".join(map(str, k["lens"])))
+def test_append(S, dtype, store, kw):
+    banner(f"append {dtype} {store} {kw}")
+    _check_append(S, Case(dtype, store, **kw, seed=_seed(dtype, store, str(kw))))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_of_extreme_rows(S, dtype):
+    """Zeros, subnormals, the largest values, infinities, NaN, ties of the rounding, and rows just at and
+    above 448 * 2^n: the same codes as the definition's."""
+    c = Case(dtype, "e4m3", [64], [64], dim=64, kv_heads=1, group=1)
+    big = torch.finfo(TORCH[dtype]).max
+    x = c.k.float()
+    x[0] = 0.0
+    x[1] = -0.0
+    x[2, 0, :] = 1e-40
+    x[3, 0, :4] = torch.tensor([big, -big, 1.0, 0.0])
+    x[4, 0, 5] = math.inf
+    x[5, 0, 6] = math.nan
+    x[6] = math.nan
+    x[7] = -math.inf
+    x[8] = torch.arange(64) * 7.0                   # up to 441: every code's neighbourhood
+    x[9] = torch.cat([torch.tensor([448.0]), 17.0 * 2.0 ** torch.arange(-31.0, 32.0).clamp(max=4)])[:64]   # ties
+    x[10] = torch.cat([torch.tensor([449.0 if dtype == "f32" else 450.0]), torch.linspace(-440, 440, 63)])
+    x[11] = 2.0 ** -10 * torch.arange(64)           # below the smallest step once 448 is there
+    x[11, 0, 63] = 448.0
+    x[12, 0, :] = 2.0 ** -126
+    c.k = x.to(TORCH[dtype])
+    _check_append(S, c)
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+def test_append_leaves_bad_places_alone(S, dtype, store):
+    """A page outside the pool, positions below 0 and behind the table: not written, flagged."""
+    banner(f"bad places {dtype} {store}")
+    c = Case(dtype, store, [40, 3], [10, 3])
+    c.table[0, 1], c.table[0, 2] = -1, c.n_pages
+    _check_append(S, c, bits=8)
+    c = Case(dtype, store, [3, 5], [6, 2])             # three tokens stand before the sequence
+    _check_append(S, c, bits=8)
+    c = Case(dtype, store, [20], [8])
+    cache, ws = c.cache(S), c.workspace(S)
+    cache.seq_len.fill_(c.max_pages * c.page + 4)      # the last four have no page
+    cache.page_table.fill_(1)
+    S.page_append(c.dims(S), cache, c.k.cuda(), c.v.cuda(), c.tok_start(), ws)
+    assert ws.status() == 8 and ws.status() == 0
+    codes, e = encode_rows(c.k) if store == "e4m3" else (c.k, None)
+    at = torch.arange(12, 16)
+    got = cache.k_pages.cpu()
+    got = got.view(torch.uint8) if store == "e4m3" else got
+    assert torch.equal(got[1, :, at].transpose(0, 1), codes[:4])
+    keep = torch.arange(12)
+    assert torch.equal(got[1, :, keep], (c.codes["k"][0])[1, :, keep])
+
+
+READS = [dict(lens=[1], page=16), dict(lens=[33, 0, 200], page=32, kv_heads=3, group=1),
+         dict(lens=[5, 1000], page=128, dim=128, kv_heads=1), dict(lens=[9, 31], page=1),
+         dict(lens=[2100], page=1024, dim=128)]
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+@pytest.mark.parametrize("kw", READS, ids=lambda k: "-".join(map(str, k["lens"])))
+def test_read(S, dtype, store, kw):
+    banner(f"read {dtype} {store} {kw}")
+    c = Case(dtype, store, news=[0] * len(kw["lens"]), **kw, seed=_seed(dtype, store, str(kw)))
+    cache, ws = c.cache(S), c.workspace(S)
+    for rows in sorted({1, max(c.lens) - 3, max(c.lens), max(c.lens) + 21}):
+        if rows < 1:
+            continue
+        keys = torch.full((c.B, c.Hkv, rows, c.d), -7.0, dtype=TORCH[dtype], device="cuda")
+        values = keys.clone()
+        S.page_read(c.dims(S), cache, rows, ws, keys=keys, values=values)
+        for name, got in (("k", keys), ("v", values)):
+            want = torch.full(got.shape, -7.0, dtype=torch.float64)
+            for b in range(c.B):
+                for g in range(c.Hkv):
+                    n = min(c.lens[b], rows)
+                    want[b, g, :n] = c.dense(name, b, g)[0][:n]
+            assert torch.equal(got.cpu().double(), want), (rows, name)
+    assert ws.status() == 0
+
+
+def test_read_skips_bad_pages(S):
+    c = Case("bf16", "e4m3", [40, 20], [0, 0])
+    c.table[0, 1], c.table[1, 0] = c.n_pages, -5
+    cache, ws = c.cache(S), c.workspace(S)
+    keys, values = S.page_read(c.dims(S), cache, 48, ws)
+    assert ws.status() == 8
+    for got, name in ((keys, "k"), (values, "v")):
+        for b, g in ((0, 0), (0, 1), (1, 0), (1, 1)):
+            x, ok = c.dense(name, b, g)
+            x[~ok] = 0.0
+            assert torch.equal(got[b, g, :c.lens[b]].cpu().double(), x)
+            assert not got[b, g, c.lens[b]:].any()
+
+
+def _attend(S, c, **kw):
+    cache, ws = c.cache(S), c.workspace(S)
+    q = c.q.to("cuda") if c.q.is_contiguous() else _strided(c, "q")
+    out = torch.full((c.total, c.Hkv * c.G, c.d), 3.0, dtype=TORCH[c.dtype], device="cuda")
+    lse = torch.full((c.total, c.Hkv * c.G), 5.0, dtype=torch.float32, device="cuda")
+    S.page_attend(c.dims(S), cache, q, c.tok_start(), ws, out=out, lse=lse)
+    torch.cuda.synchronize()
+    return out.cpu(), lse.cpu(), ws.status()
+
+
+def _check_attend(S, c, bits=0):
+    out, lse, status = _attend(S, c)
+    ref, rl, tol, ltol = c.attend()
+    n = c.start[-1]
+    err, lerr = (out.double() - ref).abs()[:n], (lse.double() - rl)[:n]
+    ratio = (err / tol[:n].clamp(min=1e-300)).max().item() if n else 0.0
+    empty = rl[:n] == -math.inf
+    assert torch.equal(lse[:n] == -math.inf, empty)
+    lratio = (lerr[~empty].abs() / ltol[:n][~empty]).max().item() if (~empty).any() else 0.0
+    banner(f"  error / bound: out {ratio:.3f}, lse {lratio:.3f}")
+    assert ratio <= 1.0 and lratio <= 1.0
+    assert not out[:n][empty].any()
+    assert (out[n:] == 3.0).all() and (lse[n:] == 5.0).all()       # rows behind the last sequence
+    assert status == bits
+
+
+ATTENDS = [
+    dict(lens=[1], news=[1]),
+    dict(lens=[2, 1, 0, 65], news=[1, 1, 0, 1], group=1, kv_heads=3),
+    dict(lens=[63, 64, 65, 129], news=[1, 1, 1, 1], group=8, kv_heads=1),
+    dict(lens=[1000, 3, 517], news=[1, 1, 1], dim=128, page=64),
+    dict(lens=[300, 40], news=[4, 2], group=4, dim=128, page=32, strided=True),
+    dict(lens=[300, 17, 90], news=[5, 17, 0], group=8, dim=64, page=8),
+    dict(lens=[200, 160], news=[33, 160], group=4, dim=128, page=16, tail=3),
+    dict(lens=[131], news=[131], group=1, kv_heads=2, page=128),
+    dict(lens=[3, 70], news=[5, 90], group=2),                             # rows before the first token
+    dict(lens=[700], news=[150], group=2, dim=128, page=256, window=100),
+    dict(lens=[260, 99], news=[1, 20], group=4, window=1),
+    dict(lens=[600, 90, 40], news=[1, 3, 40], group=4, dim=128, window=65, page=4),
+    dict(lens=[5000], news=[1], group=4, kv_heads=1, dim=128, page=64),
+    dict(lens=[2500, 31], news=[20, 31], group=4, kv_heads=1, dim=64, page=16, strided=True),
+    dict(lens=[40, 30], news=[3, 30], group=2, page=1),
+    dict(lens=[70, 41], news=[1, 37], group=4, dim=128, spread=8.0),       # weights of one entry almost
+]
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+@pytest.mark.parametrize("kw", ATTENDS, ids=lambda k: f"{k['lens']}{k['news']}".replace(" ", ""))
+def test_attend(S, dtype, store, kw):
+    banner(f"attend {dtype} {store} {kw}")
+    _check_attend(S, Case(dtype, store, **kw, seed=_seed(dtype, store, str(kw))))
+
+
+def _poison(c, b, t, value, which="kv"):
+    """Token t of sequence b holds `value` (all heads)."""
+    page, slot = int(c.table[b, t // c.page]), t % c.page
+    for name in which:
+        codes, e = c.codes[name]
+        if e is None:
+            codes[page, :, slot] = value
+        else:
+            codes[page, :, slot] = 0x7f
+        c.pools[name][page, :, slot] = value if e is None else math.nan
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("news,group", [([1, 1], 4), ([40, 6], 4), ([150, 33], 1)])
+def test_what_is_not_seen_does_not_reach_a_query(S, dtype, store, value, news, group):
+    """NaN and infinities behind the last token, outside the window, and in later tokens of the chunk: every
+    query that does not see them has the value it has without them."""
+    lens, window = [200, 77], 60
+    c = Case(dtype, store, lens, news, group=group, dim=128, page=32, window=window, seed=_seed(news, group))
+    for b, n in enumerate(lens):                     # free slots of the last pages, and unused pages
+        p = int(c.table[b, (n - 1) // c.page])
+        for name in "kv":
+            c.codes[name][0][p, :, n % c.page:] = 0x7f if store == "e4m3" else value
+    used = set(c.table[c.table < c.n_pages].tolist())
+    for p in set(range(c.n_pages)) - used:
+        for name in "kv":
+            c.codes[name][0][p] = 0x7f if store == "e4m3" else value
+    _check_attend(S, c)
+    # a token in the middle of the chunk, and one that only a part of the queries' windows reaches
+    for b, t in ((0, lens[0] - 1 - news[0] // 2), (0, lens[0] - news[0] - window + 1), (1, lens[1] - news[1])):
+        if t < 0:
+            continue
+        d = Case(dtype, store, lens, news, group=group, dim=128, page=32, window=window, seed=_seed(news, group))
+        ref, rl, tol, ltol = d.attend()
+        _poison(d, b, t, value)
+        out, lse, _ = _attend(S, d)
+        for i in range(d.total):
+            sb = 0 if i < d.start[1] else 1
+            p = lens[sb] - news[sb] + i - d.start[sb]
+            sees = sb == b and t <= p and t > p - window
+            if sees:
+                assert not torch.isfinite(out[i]).any(), (b, t, i)
+            else:
+                assert ((out[i].double() - ref[i]).abs() <= tol[i]).all(), (b, t, i)
+                assert ((lse[i].double() - rl[i]).abs() <= ltol[i]).all(), (b, t, i)
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+def test_attend_skips_bad_pages(S, dtype, store):
+    """Keys on pages outside the pool are not seen; the call flags them."""
+    for news in ([1, 1], [70, 5]):
+        c = Case(dtype, store, [200, 40], news, dim=128, page=16, seed=3)
+        c.table[0, 2], c.table[0, 5], c.table[1, 0] = -1, c.n_pages, 2 ** 31 - 1
+        _check_attend(S, c, bits=8)
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+def test_same_bits_again_and_on_another_stream(S, dtype, store):
+    c = Case(dtype, store, [3000, 70, 9], [1, 33, 2], dim=128, kv_heads=1, group=4, page=16, seed=11)
+    cache, ws, q, ts = c.cache(S), c.workspace(S), c.q.cuda(), c.tok_start()
+    a, la = S.page_attend(c.dims(S), cache, q, ts, ws, want_lse=True)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    b, lb = S.page_attend(c.dims(S), cache, q, ts, ws, want_lse=True, stream=st)
+    st.synchronize()
+    assert torch.equal(a, b) and torch.equal(la, lb)
+    assert S.page_attend(c.dims(S), cache, q, ts, ws)[1] is None
