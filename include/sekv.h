@@ -363,7 +363,8 @@ typedef struct {
     int32_t n_q_heads;      /* Hq; query head h reads KV head h / (Hq / Hkv)               */
     int32_t n_kv_heads;     /* Hkv; Hq / Hkv in {1, 2, 4, 8}                               */
     int32_t head_dim;       /* d in {64, 128}                                              */
-    int32_t page_size;      /* tokens a page: a power of two, 1..1024                      */
+    int32_t page_size;      /* tokens a page: a power of two, 16..1024 (16 keys fill a     
+                               matrix tile's side)                                         */
     int32_t n_pages;        /* pages in the pool, n_pages * Hkv * page_size < 2^31         */
     int32_t max_pages;      /* row stride of the page table, max_pages * page_size <= 2^30 */
     int32_t dtype;          /* SEKV_F32 or SEKV_BF16: new tokens, queries, outputs          */
@@ -373,7 +374,7 @@ typedef struct {
     double softmax_scale;
 } sekv_page_dims;
 
-/* One layer's pages.  Device pointers, caller-owned; pools 16-byte aligned. */
+/* One layer's pages.  Device pointers, caller-owned; pools and scales 16-byte aligned. */
 typedef struct {
     void *k;                /* [n_pages][Hkv][page_size][d] in page_dtype                  */
     void *v;

@@ -28,6 +28,8 @@ DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                 "-Xarch_device", "-Wframe-larger-than=0", "-Xarch_device", "-Werror=frame-larger-than"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", f"-I{INCLUDE}", f"-I{CSRC}"]
 SVD_INSTANCES = [(2, 128), (4, 128), (2, 64), (4, 64)]      # (element bytes, head_dim)
+PAGE_INSTANCES = [("BF16", "BF16", 128), ("BF16", "E4M3", 128), ("BF16", "BF16", 64), ("BF16", "E4M3", 64),
+                  ("F32", "F32", 128), ("F32", "E4M3", 128), ("F32", "F32", 64), ("F32", "E4M3", 64)]
 INSTANCES = [("BF16", 128), ("BF16", 64), ("F32", 128), ("F32", 64)]
 
 # every source the kernels are built from (the bench hashes these to tie counter
@@ -55,11 +57,14 @@ def _jobs(bdir, trace):
         jobs.append(([HIPCC, *COMMON, f"--offload-arch={ARCH}", *DEVICE_FLAGS, *tflag,
                       f"-DSEKV_T={t}", f"-DSEKV_D={d}", "-c",
                       os.path.join(CSRC, "sekv_step_inst.hip"), "-o", obj], obj))
-    for src in ("sekv_kernels.hip", "sekv_tier.hip", "sekv_noalloc.hip", "sekv_gate.hip", "sekv_page.hip",
-                "sekv_page_attend.hip"):
+    for src in ("sekv_kernels.hip", "sekv_tier.hip", "sekv_noalloc.hip", "sekv_gate.hip", "sekv_page.hip"):
         obj = os.path.join(bdir, src.replace(".hip", ".o"))
         jobs.append(([HIPCC, *COMMON, f"--offload-arch={ARCH}", *DEVICE_FLAGS, "-c",
                       os.path.join(CSRC, src), "-o", obj], obj))
+    for t, p, d in PAGE_INSTANCES:
+        obj = os.path.join(bdir, f"sekv_page_attend_{t}_{p}_{d}.o")
+        jobs.append(([HIPCC, *COMMON, f"--offload-arch={ARCH}", *DEVICE_FLAGS, f"-DSEKV_T={t}", f"-DSEKV_P={p}",
+                      f"-DSEKV_D={d}", "-c", os.path.join(CSRC, "sekv_page_attend_inst.hip"), "-o", obj], obj))
     obj = os.path.join(bdir, "sekv_build.o")
     jobs.append(([HIPCC, *COMMON, f"--offload-arch={ARCH}", *DEVICE_FLAGS, "-c",
                   os.path.join(CSRC, "sekv_build.hip"), "-o", obj], obj))

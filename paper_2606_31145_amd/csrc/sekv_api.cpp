@@ -178,6 +178,16 @@ void ws_note_zeroed(void *ws, size_t bytes) {
     g_ws.zeroed(reinterpret_cast<uintptr_t>(ws), bytes);
 }
 
+}  // namespace
+namespace sekv {
+// A call with no layout of its own state has written over a workspace: the next step zeroes it.
+void note_foreign_use(void *ws, size_t bytes) {
+    std::lock_guard<std::mutex> lk(g_ws_mu);
+    (void)g_ws.before_launch(reinterpret_cast<uintptr_t>(ws), bytes, ~uint64_t(0), 1);
+}
+}  // namespace sekv
+namespace {
+
 hipError_t ws_prepare(void *ws, size_t ws_bytes, uint64_t key, uint64_t n_launch, hipStream_t stream) {
     std::lock_guard<std::mutex> lk(g_ws_mu);
     if (g_ws.before_launch(reinterpret_cast<uintptr_t>(ws), ws_bytes, key, n_launch))

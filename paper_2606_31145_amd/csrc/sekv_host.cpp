@@ -315,8 +315,8 @@ sekv_status check_page_dims(const sekv_page_dims *d) {
     if (d->n_q_heads > 4096) return fail(SEKV_ERR_UNSUPPORTED, "n_q_heads %d > 4096", d->n_q_heads);
     if (d->head_dim != 64 && d->head_dim != 128)
         return fail(SEKV_ERR_UNSUPPORTED, "head_dim %d not in {64,128}", d->head_dim);
-    if (d->page_size < 1 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)))
-        return fail(SEKV_ERR_UNSUPPORTED, "page_size %d: a power of two in [1, 1024]", d->page_size);
+    if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)))
+        return fail(SEKV_ERR_UNSUPPORTED, "page_size %d: a power of two in [16, 1024]", d->page_size);
     if (d->n_pages < 1 || d->max_pages < 1)
         return fail(SEKV_ERR_INVALID_ARG, "n_pages/max_pages < 1");
     if ((long long)d->n_pages * d->n_kv_heads * d->page_size > 0x7fffffffll)
@@ -348,6 +348,8 @@ sekv_status check_pages(const sekv_page_dims *d, const sekv_pages *p) {
         return fail(SEKV_ERR_INVALID_ARG, "pages.k_scale or v_scale is NULL");
     if (!e4m3 && (p->k_scale || p->v_scale))
         return fail(SEKV_ERR_INVALID_ARG, "scales given for pages without them");
+    if (misaligned(p->k_scale, 16) || misaligned(p->v_scale, 16))
+        return fail(SEKV_ERR_INVALID_ARG, "page scales not 16-byte aligned");
     return SEKV_OK;
 }
 

@@ -12,6 +12,17 @@
 #include "sekv_page_row.h"
 
 namespace sekv {
+
+// defined in sekv_page_attend_inst.hip, one object per (token type, storage type, head_dim)
+hipError_t launch_page_attend_BF16_BF16_128(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_BF16_BF16_64(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_BF16_E4M3_128(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_BF16_E4M3_64(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_F32_F32_128(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_F32_F32_64(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_F32_E4M3_128(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_F32_E4M3_64(const PageAttendArgs &a, hipStream_t s);
+
 namespace {
 
 using namespace page;
@@ -179,6 +190,16 @@ hipError_t launch_page_append(const PageAppendArgs &a, int dtype, int page_dtype
 
 hipError_t launch_page_read(const PageReadArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream) {
     return dispatch(dtype, page_dtype, head_dim, [&](auto t, auto p, auto d) { return read<decltype(t), decltype(p), decltype(d)::value>(a, stream); });
+}
+
+hipError_t launch_page_attend(const PageAttendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t s) {
+    const bool q = page_dtype == SEKV_E4M3;
+    if (dtype == SEKV_BF16) {
+        if (head_dim == 128) return q ? launch_page_attend_BF16_E4M3_128(a, s) : launch_page_attend_BF16_BF16_128(a, s);
+        return q ? launch_page_attend_BF16_E4M3_64(a, s) : launch_page_attend_BF16_BF16_64(a, s);
+    }
+    if (head_dim == 128) return q ? launch_page_attend_F32_E4M3_128(a, s) : launch_page_attend_F32_F32_128(a, s);
+    return q ? launch_page_attend_F32_E4M3_64(a, s) : launch_page_attend_F32_F32_64(a, s);
 }
 
 }  // namespace sekv

@@ -7,6 +7,7 @@
 #include "sekv.h"
 #include "sekv_host.h"
 #include "sekv_internal.h"
+#include "sekv_page_index.h"
 #include "sekv_page_internal.h"
 
 namespace {
@@ -64,7 +65,21 @@ sekv::PageTables tables(const sekv_page_dims *d, const sekv_pages *p, const int3
     return t;
 }
 
-size_t workspace_bytes(const sekv_page_dims *, int32_t) { return sizeof(sekv::WsHeader); }
+// Work items that fill the device: two workgroups a compute unit, four rounds of them, so that
+// ragged chunks even out.
+constexpr int kItems = 2048;
+
+sekv::page::Launch plan(const sekv_page_dims *d, int n_tokens) {
+    return sekv::page::plan_launch(d->batch, n_tokens, d->n_kv_heads, log2_of(d->n_q_heads / d->n_kv_heads),
+                                   int64_t(d->max_pages) * d->page_size, kItems);
+}
+
+// The header, then the partials of split tiles.
+size_t workspace_bytes(const sekv_page_dims *d, int32_t n_tokens) {
+    const int64_t rows = sekv::page::partial_rows(n_tokens, d->n_kv_heads, log2_of(d->n_q_heads / d->n_kv_heads),
+                                                  int64_t(d->max_pages) * d->page_size, kItems);
+    return sizeof(sekv::WsHeader) + size_t(rows) * (d->head_dim + 2) * sizeof(float);
+}
 
 }  // namespace
 
@@ -130,8 +145,7 @@ sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages
                              size_t ws_bytes, hipStream_t stream) {
     if (n_tokens < 0) return fail(SEKV_ERR_INVALID_ARG, "n_tokens < 0");
     bool go = false;
-    sekv_status st = check_call(dims, pages, ws, ws_bytes, dims ? workspace_bytes(dims, n_tokens) : 0,
-                                n_tokens == 0, &go);
+    sekv_status st = check_call(dims, pages, ws, ws_bytes, sizeof(sekv::WsHeader), n_tokens == 0, &go);
     if (st != SEKV_OK || !go) return st;
     if (!tok_start || misaligned(tok_start, 4))
         return fail(SEKV_ERR_INVALID_ARG, "tok_start is NULL or not 4-byte aligned");
@@ -140,6 +154,8 @@ sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages
     if (misaligned(lse, 4)) return fail(SEKV_ERR_INVALID_ARG, "lse not 4-byte aligned");
     if (int64_t(n_tokens) * dims->n_q_heads > 0x7fffffffll)
         return fail(SEKV_ERR_UNSUPPORTED, "%d new tokens of %d heads in one call", n_tokens, dims->n_q_heads);
+    if (ws_bytes < workspace_bytes(dims, n_tokens))
+        return fail(SEKV_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, workspace_bytes(dims, n_tokens));
     sekv::PageAttendArgs a{};
     a.t = tables(dims, pages, tok_start, n_tokens, ws);
     a.q = q; a.q_stride = q_stride;
@@ -148,7 +164,12 @@ sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages
     a.out = out; a.lse = lse;
     a.group_shift = log2_of(dims->n_q_heads / dims->n_kv_heads);
     a.window = dims->window > 0 ? dims->window : 0x7fffffff;
-    a.scale = float(dims->softmax_scale);
+    a.scale_log2 = float(dims->softmax_scale * 1.4426950408889634074);
+    const sekv::page::Launch l = plan(dims, n_tokens);
+    a.splits = l.splits; a.target = l.target; a.pairs = l.pairs;
+    a.part_o = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + sizeof(sekv::WsHeader));
+    a.part_ml = a.part_o + size_t(l.splits) * n_tokens * dims->n_q_heads * dims->head_dim;
+    sekv::note_foreign_use(ws, ws_bytes);
     const hipError_t e = sekv::launch_page_attend(a, dims->dtype, dims->page_dtype, dims->head_dim, stream);
     if (e != hipSuccess) return fail(SEKV_ERR_HIP, "page attention launch: %s", hipGetErrorString(e));
     return SEKV_OK;

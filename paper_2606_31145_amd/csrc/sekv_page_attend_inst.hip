@@ -1,0 +1,231 @@
+// Attention of new tokens over the paged store, one pair of storage types and head_dim an object.
+//
+// softmax in one pass: with m a bound of the scores so far, l = sum exp(s - m) and o = sum exp(s - m) v,
+// a larger m scales l and o by exp(old - new).  A workgroup takes one item (sekv_page_index.h): a tile
+// of query rows of one sequence and KV head against a chunk of its keys.  A tile whose keys lie in more
+// than one chunk leaves partials (m, l, o), which a second kernel joins.
+#include <hip/hip_runtime.h>
+
+#include "sekv_page_wide.h"
+
+#if !defined(SEKV_T) || !defined(SEKV_P) || !defined(SEKV_D)
+#error "build with -DSEKV_T=BF16|F32 -DSEKV_P=BF16|F32|E4M3 -DSEKV_D=64|128"
+#endif
+
+namespace sekv {
+namespace {
+
+using namespace page;
+
+constexpr int kThreads = 256, kWaves = 4;
+
+// At most 16 rows: every wave takes all of them, and every fourth step of the keys.  True when the item
+// has to be done again by plain_rows.
+template <class T, class P, int D>
+__device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
+    using R = Rows16<T, P, D, 1>;
+    constexpr int VE = R::VE, RS = D + 4, kKeys = R::Tile::kKeys;
+    R r;
+    r.init(a, it, g, 0, lane);
+    bool bad = false;
+    r.run(a, it, b, g, it.begin + wave * kKeys, kKeys * kWaves, &bad, lane);
+    // the four waves' parts, joined through LDS
+    float *ml = reinterpret_cast<float *>(lds), *so = ml + kWaves * 32;
+    const int n = lane & 15, gq = lane >> 4;
+    const float l = r.sum(0);
+    if (gq == 0) {
+        ml[wave * 32 + n] = r.m[0];
+        ml[wave * 32 + 16 + n] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) so[(wave * 16 + n) * RS + VE * (4 * gq + i) + e] = r.o[0][e][i];
+    if (__syncthreads_or(bad)) return true;
+    const int rw = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VE;
+    if (rw < it.rows) {
+        float m = -INFINITY, sum = 0.f, o[VE] = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w * 32 + rw]);
+        const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = exp2_fast(ml[w * 32 + rw] - mu);
+            sum += f * ml[w * 32 + 16 + rw];
+#pragma unroll
+            for (int e = 0; e < VE; ++e) o[e] += f * so[(w * 16 + rw) * RS + d0 + e];
+        }
+        put<T, D>(a, it, c, it.tok0 + (rw >> a.group_shift), (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1)), d0, o, m, sum);
+    }
+    return false;
+}
+
+// Up to 128 float rows: 32 to a wave, which reads all the item's keys.
+template <class P, int D>
+__device__ inline bool wide_f32(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave) {
+    using R = Rows16<F32, P, D, 2>;
+    R r;
+    bool bad = false;
+    if (wave * 32 < it.rows) {
+        r.init(a, it, g, wave * 32, lane);
+        r.run(a, it, b, g, it.begin, 16, &bad, lane);
+    }
+    if (__syncthreads_or(bad)) return true;
+    if (wave * 32 >= it.rows) return false;
+    const int n = lane & 15, gq = lane >> 4;
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+        const int rw = wave * 32 + nb * 16 + n;
+        const float l = r.sum(nb);
+        if (rw < it.rows) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float o[R::VE];
+#pragma unroll
+                for (int e = 0; e < R::VE; ++e) o[e] = r.o[nb][e][i];
+                put<F32, D>(a, it, c, it.tok0 + (rw >> a.group_shift), (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1)),
+                            R::VE * (4 * gq + i), o, r.m[nb], l);
+            }
+        }
+    }
+    return false;
+}
+
+// Up to 128 bfloat16 rows: tiles of 64 keys in LDS, two buffers; a wave fetches 16 keys of each.
+template <class P, int D>
+__device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
+    constexpr int kTile = 64 * D * 2;                        // bytes of a tile's keys or values
+    Rows32<D> r;
+    r.init(a, it, g, wave * 32, lane);
+    const int64_t w = it.p0 + it.n_tok - 1 - (int64_t(a.window) - 1);
+    const int64_t all_lo = w, all_hi = it.p0;                // keys that every row of the item sees
+    Stage<P, D> st;
+    bool bad = false;
+    // the four blocks of a tile: mine to fetch, all of them to know which hold keys
+    auto look = [&](int pos, int *mine) {
+        uint32_t valid = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = key_block(a, b, g, pos + 16 * j, it.end, lane);
+            valid |= row >= 0 ? 1u << j : 0u;
+            if (j == wave) *mine = row;
+        }
+        return valid;
+    };
+    auto store = [&](int pos, uint32_t valid, int buf) {
+        if (valid != 15u || pos < all_lo || pos + 63 > all_hi)
+            bad |= st.mend(wave * 16, valid >> wave & 1 ? it.end - pos : 0, lane);
+        st.store(lds + buf * kTile, lds + (2 + buf) * kTile, wave * 16, lane);
+    };
+    int mine = -1;
+    uint32_t valid = look(it.begin, &mine);
+    st.load(a, mine, lane);
+    uint32_t ahead = look(it.begin + 64, &mine);
+    int buf = 0;
+    store(it.begin, valid, 0);
+    __syncthreads();
+    for (int pos = it.begin; pos < it.end; pos += 64) {
+        const bool more = pos + 64 < it.end;
+        uint32_t after = 0;
+        if (more) {
+            st.load(a, mine, lane);
+            after = look(pos + 128, &mine);
+        }
+        r.step(a, lds + buf * kTile, lds + (2 + buf) * kTile, pos, valid, lane);
+        buf ^= 1;
+        if (more) store(pos + 64, ahead, buf);
+        __syncthreads();
+        valid = ahead;
+        ahead = after;
+    }
+    if (__syncthreads_or(bad)) return true;
+    const int n = lane & 31, h = lane >> 5, rw = wave * 32 + n;
+    const float l = r.l + across32(r.l);
+    if (rw < it.rows) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float o[4] = {r.o[db][4 * i], r.o[db][4 * i + 1], r.o[db][4 * i + 2], r.o[db][4 * i + 3]};
+                put<BF16, D>(a, it, c, it.tok0 + (rw >> a.group_shift), (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1)),
+                             32 * db + 8 * i + 4 * h, o, r.m, l);
+            }
+    }
+    return false;
+}
+
+template <class T, class P, int D>
+__global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
+    constexpr int kNarrowLds = (kWaves * 32 + kWaves * 16 * (D + 4)) * 4, kWideLds = T::kBytes == 2 ? 4 * 64 * D * 2 : 0;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[kNarrowLds > kWideLds ? kNarrowLds : kWideLds];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (blockIdx.x == 0)                                     // tables that cannot be
+        for (int b = threadIdx.x; b < a.t.B; b += kThreads) {
+            const Seq s = load_seq(a, b);
+            const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
+            if (a.t.tok_start[b] != s.start || a.t.tok_start[b + 1] != s.start + s.nq || a.t.seq_len[b] < 0 ||
+                (s.nq && a.t.seq_len[b] > cap))
+                flag(a.t);
+        }
+    const int g = blockIdx.x % a.t.Hkv, chunk = find_chunk(a, lane);
+    int b = 0, c = 0;
+    Item it;
+    if (!find_item(a, blockIdx.x / a.t.Hkv, lane, chunk, &b, &c, &it)) return;
+    bool again;
+    if (it.narrow) again = narrow<T, P, D>(a, it, b, g, c, lane, wave, lds);
+    else if constexpr (T::kBytes == 2) again = wide_bf16<P, D>(a, it, b, g, c, lane, wave, lds);
+    else again = wide_f32<P, D>(a, it, b, g, c, lane, wave);
+    if (again) plain_rows<T, P, D>(a, it, b, g, c, lane, wave);
+}
+
+// Joins the partials of one token and head: one wave, the lanes over d.
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
+    const int lane = threadIdx.x & 63, Hq = a.t.Hkv << a.group_shift;
+    const int64_t row = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const int tok = __builtin_amdgcn_readfirstlane(int(row / Hq)), h = int(row % Hq);
+    if (tok >= a.t.n_tokens) return;
+    const int chunk = find_chunk(a, lane);
+    int lo = 0, hi = a.t.B;                                  // the last b with tok_start[b] <= tok
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.t.tok_start[mid] <= tok) lo = mid; else hi = mid;
+    }
+    const Seq s = load_seq(a, lo);
+    if (tok < s.start || tok >= s.start + s.nq) return;
+    const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
+    const int tile = (s.nq << a.group_shift) <= kNarrowRows ? 0 : ((tok - s.start) << a.group_shift) / kTileRows;
+    Item it = make_item(s, tile, 0, chunk, cap, a.window, a.group_shift);
+    if (it.chunk0 == it.chunk1) return;
+    float m = -INFINITY, l = 0.f, o[D / 64] = {};
+    const size_t step = size_t(a.t.n_tokens) * Hq, at0 = size_t(tok) * Hq + h;
+    for (int c = it.chunk0; c <= it.chunk1; ++c) m = fmaxf(m, a.part_ml[2 * (c * step + at0)]);
+    const float mu = m == -INFINITY ? 0.f : m;
+    for (int c = it.chunk0; c <= it.chunk1; ++c) {
+        const size_t at = c * step + at0;
+        const float f = exp2_fast(a.part_ml[2 * at] - mu);
+        l += f * a.part_ml[2 * at + 1];
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) o[i] += f * a.part_o[at * D + lane * (D / 64) + i];
+    }
+    it.chunk0 = it.chunk1;
+    put<T, D>(a, it, 0, tok, h, lane * (D / 64), o, m, l);
+}
+
+}  // namespace
+
+#define SEKV_NAME2(t, p, d) launch_page_attend_##t##_##p##_##d
+#define SEKV_NAME(t, p, d) SEKV_NAME2(t, p, d)
+
+hipError_t SEKV_NAME(SEKV_T, SEKV_P, SEKV_D)(const PageAttendArgs &a, hipStream_t s) {
+    using T = page::SEKV_T;
+    using P = page::SEKV_P;
+    hipLaunchKernelGGL((attend_kernel<T, P, SEKV_D>), dim3(unsigned(a.pairs * a.t.Hkv)), dim3(kThreads), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t rows = int64_t(a.t.n_tokens) * (a.t.Hkv << a.group_shift);
+    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace sekv

@@ -1,0 +1,140 @@
+// Where a row of the paged store lies, and which workgroup of sekv_page_attend does what: integer
+// arithmetic only, also compiled for the host, where a test walks through it.
+//
+// Work items.  The query rows of a sequence and KV head (its new tokens x its query heads) are cut
+// into tiles of kTileRows, or are one narrow tile when there are at most kNarrowRows.  A tile's keys
+// are cut into chunks so that few rows over many keys still fill the device.  The chunk length is
+// found from the device's tables, the same for the whole call: with T_b tiles and L_b keys of
+// sequence b, W = sum T_b L_b, chunk = max(W / target, max L_b / splits) in steps of kChunkStep
+// keys.  Then there are at most sum T_b + target (tile, chunk) pairs, whatever the lengths: the grid
+// can be sized before they are known, and no sequence gets more than `splits` chunks.
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define SEKV_HD __host__ __device__ inline
+#else
+#define SEKV_HD inline
+#endif
+
+namespace sekv {
+namespace page {
+
+constexpr int kNarrowRows = 16;    // columns of a 16-wide matrix tile
+constexpr int kTileRows = 128;     // 32 rows for each of four waves
+constexpr int kChunkStep = 256;    // keys: a step of 64 for each of four waves
+constexpr int kBlock = 16;         // keys that lie in one page: the smallest page
+
+// Pool row of position `pos` (below max_pages * page_size) from its table entry; -1 when the page is
+// outside the pool.  The kBlock positions from a multiple of kBlock on are consecutive rows.
+SEKV_HD int block_row(int page, int n_pages, int Hkv, int g, int page_shift, int pos) {
+    if (uint32_t(page) >= uint32_t(n_pages)) return -1;
+    return ((page * Hkv + g) << page_shift) | (pos & ((1 << page_shift) - 1));
+}
+
+// One sequence of a call.  Positions stay what seq_len says; only keys are cut off at the capacity.
+struct Seq {
+    int start, nq;        // its rows of the new tokens
+    int64_t first;        // position of the first new token (may be negative)
+    int lo, len;          // keys lo .. lo + len - 1 are seen by some query; lo a multiple of kChunkStep
+    int tiles;
+};
+
+SEKV_HD Seq make_seq(int start, int end, int seq_len, int n_tokens, int64_t cap, int window, int group_shift) {
+    Seq s;
+    start = start < 0 ? 0 : start > n_tokens ? n_tokens : start;
+    end = end < start ? start : end > n_tokens ? n_tokens : end;
+    s.start = start;
+    s.nq = end - start;
+    const int n = seq_len < 0 ? 0 : seq_len;
+    s.first = int64_t(n) - s.nq;
+    int64_t lo = s.first - (int64_t(window) - 1), hi = n < cap ? n : cap;
+    lo = lo < 0 ? 0 : lo / kChunkStep * kChunkStep;
+    s.lo = int(lo < hi ? lo : 0);
+    s.len = s.nq && lo < hi ? int(hi - lo) : 0;
+    const int rows = s.nq << group_shift;
+    s.tiles = rows <= kNarrowRows ? (rows > 0) : (rows + kTileRows - 1) / kTileRows;
+    return s;
+}
+
+SEKV_HD int chunk_length(uint64_t W, int max_len, int target, int splits) {
+    uint64_t c = (W + target - 1) / uint64_t(target);
+    const uint64_t d = (uint64_t(max_len) + splits - 1) / uint64_t(splits);
+    c = c > d ? c : d;
+    c = (c + kChunkStep - 1) / kChunkStep * kChunkStep;
+    return int(c < kChunkStep ? kChunkStep : c > (1u << 30) ? (1u << 30) : c);
+}
+SEKV_HD int chunks_of(const Seq &s, int chunk) { return s.len > chunk ? (s.len + chunk - 1) / chunk : 1; }
+
+// What one item covers.
+struct Item {
+    int tok0, n_tok;      // tokens of the tile
+    int rows;             // n_tok << group_shift
+    bool narrow;
+    int64_t p0;           // position of its first token
+    int begin, end;       // keys (begin a multiple of 64); empty when begin >= end
+    int chunk0, chunk1;   // first and last chunk with keys of the tile; equal: no join is needed
+    bool idle;            // nothing to do
+};
+
+SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, int window, int group_shift) {
+    Item it;
+    it.narrow = (s.nq << group_shift) <= kNarrowRows;
+    const int per = it.narrow ? s.nq : kTileRows >> group_shift;
+    const int t0 = tile * per, left = s.nq - t0;
+    it.tok0 = s.start + t0;
+    it.n_tok = left < per ? left : per;
+    it.rows = it.n_tok << group_shift;
+    it.p0 = s.first + t0;
+    int64_t b = it.p0 - (int64_t(window) - 1), e = it.p0 + it.n_tok;
+    b = b < 0 ? 0 : b / 64 * 64;
+    e = e < 0 ? 0 : e < cap ? e : cap;
+    if (b >= e) {                                  // no key: the first chunk's item says so
+        it.begin = it.end = 0;
+        it.chunk0 = it.chunk1 = 0;
+        it.idle = c != 0;
+        return it;
+    }
+    it.chunk0 = int((b - s.lo) / chunk);
+    it.chunk1 = int((e - 1 - s.lo) / chunk);
+    it.idle = c < it.chunk0 || c > it.chunk1;
+    const int64_t cb = s.lo + int64_t(c) * chunk, ce = cb + chunk;
+    it.begin = int(b > cb ? b : cb);
+    it.end = int(e < ce ? e : ce);
+    return it;
+}
+
+// Host side: grid and workspace of a call.
+struct Launch {
+    int splits;           // chunks a tile may have
+    int target;           // (tile, chunk) pairs aimed at
+    int64_t pairs;        // (tile, chunk) pairs at most
+};
+
+SEKV_HD int most_splits(int64_t cap) {
+    const int64_t n = (cap + kChunkStep - 1) / kChunkStep;
+    return int(n > 256 ? 256 : n);
+}
+// `items`: how many work items fill the device.
+SEKV_HD Launch plan_launch(int batch, int n_tokens, int Hkv, int group_shift, int64_t cap, int items) {
+    Launch l;
+    const int64_t rows = int64_t(n_tokens) << group_shift, r = rows > kTileRows ? rows : kTileRows;
+    l.target = (items + Hkv - 1) / Hkv;
+    const int64_t s = (int64_t(l.target) * kTileRows + r - 1) / r;
+    const int most = most_splits(cap);
+    l.splits = int(s < most ? s : most);
+    const int64_t tiles = (batch < n_tokens ? batch : n_tokens) + rows / kTileRows;
+    l.pairs = tiles + (l.splits > 1 ? l.target : 0);
+    return l;
+}
+// Rows of partials (of all heads) that any call of up to n_tokens tokens needs: splits * rows is at
+// most target * kTileRows + rows, and at most most_splits * rows.
+SEKV_HD int64_t partial_rows(int n_tokens, int Hkv, int group_shift, int64_t cap, int items) {
+    const int64_t rows = int64_t(n_tokens) << group_shift, target = (items + Hkv - 1) / Hkv;
+    const int64_t a = target * kTileRows + rows, b = rows * most_splits(cap);
+    return (a < b ? a : b) * Hkv;
+}
+
+}  // namespace page
+}  // namespace sekv

@@ -53,8 +53,15 @@ struct PageAttendArgs {
     float *lse;                // [n_tokens][Hq] or null
     int32_t group_shift;       // log2(Hq / Hkv)
     int32_t window;            // > 0; 2^31 - 1: none
-    float scale;
+    int32_t splits, target;    // see sekv_page_index.h
+    int64_t pairs;
+    float scale_log2;          // softmax_scale * log2(e)
+    float *part_o;             // [splits][n_tokens][Hq][d]
+    float *part_ml;            // [splits][n_tokens][Hq][2]: maximum (base 2), sum
 };
+
+// sekv_api.cpp: a workspace that the step calls may share holds something else now.
+void note_foreign_use(void *ws, size_t bytes);
 
 hipError_t launch_page_append(const PageAppendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);
 hipError_t launch_page_read(const PageReadArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);

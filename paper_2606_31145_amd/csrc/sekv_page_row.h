@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "sekv_page_index.h"
 #include "sekv_page_internal.h"
 
 namespace sekv {
@@ -55,6 +56,16 @@ __device__ inline void codes4_up(uint32_t w, float scale, float (&x)[4]) {
     x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
 }
 
+// two or eight codes as bfloat16, scaled by 2^(E - 127) (exact but where bfloat16 itself ends)
+__device__ inline uint32_t codes2_bf16(uint32_t w, float scale, int high) {
+    return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))
+                : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+}
+__device__ inline uint4 codes8_bf16(uint32_t w0, uint32_t w1, float scale) {
+    return make_uint4(codes2_bf16(w0, scale, 0), codes2_bf16(w0, scale, 1), codes2_bf16(w1, scale, 0),
+                      codes2_bf16(w1, scale, 1));
+}
+
 __device__ inline void flag(const PageTables &t) {
     __hip_atomic_fetch_or(t.error, kErrPageRange, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -62,9 +73,7 @@ __device__ inline void flag(const PageTables &t) {
 // Pool row of token `pos` (0 <= pos < max_pages * page_size) of sequence b, head g; -1 when its
 // page is outside the pool.
 __device__ inline int pool_row(const PageTables &t, int b, int g, int pos) {
-    const int page = t.table[size_t(b) * t.max_pages + (pos >> t.page_shift)];
-    if (uint32_t(page) >= uint32_t(t.n_pages)) return -1;
-    return (((page * t.Hkv + g) << t.page_shift) | (pos & ((1 << t.page_shift) - 1)));
+    return block_row(t.table[size_t(b) * t.max_pages + (pos >> t.page_shift)], t.n_pages, t.Hkv, g, t.page_shift, pos);
 }
 
 }  // namespace page

@@ -1,0 +1,543 @@
+// Building blocks of sekv_page_attend on the matrix cores.
+//
+// Scores are formed transposed, S^T = K Q^T: a lane holds the scores of one query row (column
+// lane % 16 or % 32 of the result) against several keys, so the softmax's maximum and sum are per
+// lane but for one exchange between the lanes of a column, and the weights already lie as the
+// second operand of O^T += V^T P^T wants them: the contraction runs over keys in the order in which
+// the first product leaves them, and V is read in that same order.
+//
+// The running maximum is moved only when a score passes it by more than kSlack (in base 2): weights
+// then reach 2^8 at most instead of 1, which float sums do not mind, and most tiles need neither an
+// exchange nor a rescaling of the output.
+#pragma once
+
+#include "sekv_page_index.h"
+#include "sekv_page_row.h"
+
+namespace sekv {
+namespace page {
+
+typedef float f4v __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef __bf16 b8v __attribute__((ext_vector_type(8)));
+
+constexpr float kSlack = 8.f;
+
+__device__ inline f4v mma16(const uint4 &a, const uint4 &b, f4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8v, a), __builtin_bit_cast(b8v, b), c, 0, 0, 0);
+}
+__device__ inline f4v mma16(float a, float b, f4v c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+__device__ inline f16v mma32(const uint4 &a, const uint4 &b, f16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8v, a), __builtin_bit_cast(b8v, b), c, 0, 0, 0);
+}
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The value of the lane 32 or 16 away.
+__device__ inline float across32(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+__device__ inline float across16(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
+}
+
+// Is an element not finite (bfloat16 pairs; float).
+__device__ inline uint32_t odd2(uint32_t w) { return uint32_t((w & 0x7f80u) == 0x7f80u) | uint32_t((w & 0x7f800000u) == 0x7f800000u); }
+__device__ inline uint32_t odd(const uint4 &v) { return odd2(v.x) | odd2(v.y) | odd2(v.z) | odd2(v.w); }
+__device__ inline bool odd(float x) { return !(fabsf(x) <= 3.402823466e38f); }
+
+__device__ inline Seq load_seq(const PageAttendArgs &a, int b) {
+    const PageTables &t = a.t;
+    return make_seq(t.tok_start[b], t.tok_start[b + 1], t.seq_len[b], t.n_tokens, int64_t(t.max_pages) << t.page_shift,
+                    a.window, a.group_shift);
+}
+
+// The call's chunk length: two sums over the batch.
+__device__ inline int find_chunk(const PageAttendArgs &a, int lane) {
+    if (a.splits == 1) return 1 << 30;
+    uint64_t W = 0;
+    int mx = 0;
+    for (int b = lane; b < a.t.B; b += 64) {
+        const Seq s = load_seq(a, b);
+        W += uint64_t(s.tiles) * uint64_t(s.len);
+        mx = mx > s.len ? mx : s.len;
+    }
+    if (a.t.B > 1) {
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) {
+            W += __shfl_xor((unsigned long long)W, k);
+            const int y = __shfl_xor(mx, k);
+            mx = mx > y ? mx : y;
+        }
+    }
+    W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
+    return chunk_length(W, __builtin_amdgcn_readfirstlane(mx), a.target, a.splits);
+}
+
+// Pair x of the call: sequences in order, chunks of a sequence in order, tiles last first (the later
+// tokens of a chunk see more keys).
+__device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, int chunk, int *b_out, int *c_out, Item *it) {
+    const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
+    uint32_t before = 0;
+    for (int b0 = 0; b0 < a.t.B; b0 += 64) {
+        uint32_t n = 0;
+        if (b0 + lane < a.t.B) {
+            const Seq s = load_seq(a, b0 + lane);
+            n = uint32_t(s.tiles) * uint32_t(chunks_of(s, chunk));
+        }
+        uint32_t incl = n;
+        if (a.t.B > 1) {
+#pragma unroll
+            for (int k = 1; k < 64; k *= 2) {
+                const uint32_t y = __shfl_up(incl, k);
+                incl += lane >= k ? y : 0u;
+            }
+        }
+        const unsigned long long past = __ballot(before + incl > x);
+        if (past) {
+            const int l = __ffsll(past) - 1;
+            const uint32_t in = x - before - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l));
+            const int b = b0 + l;
+            const Seq s = load_seq(a, b);
+            *b_out = b;
+            *c_out = int(in / uint32_t(s.tiles));
+            *it = make_item(s, s.tiles - 1 - int(in % uint32_t(s.tiles)), *c_out, chunk, cap, a.window, a.group_shift);
+            return !it->idle;
+        }
+        before += __builtin_amdgcn_readlane(incl, 63);
+    }
+    return false;
+}
+
+// Pool row of the 16 keys at `pos` of sequence b and head g; -1 behind `end` or on a page outside the
+// pool.  Uniform in the wave: read through the scalar cache.
+__device__ inline int key_block(const PageAttendArgs &a, int b, int g, int pos, int end, int lane) {
+    if (pos >= end) return -1;
+    typedef const __attribute__((address_space(4))) int32_t *ro;
+    const int page = ((ro)(uintptr_t)a.t.table)[int64_t(b) * a.t.max_pages + (pos >> a.t.page_shift)];
+    const int r = block_row(page, a.t.n_pages, a.t.Hkv, g, a.t.page_shift, pos);
+    if (r < 0 && lane == 0) flag(a.t);
+    return r;
+}
+
+// Where a row's result goes: the output, or a partial of its chunk.  o: N consecutive values from d0
+// on, weighted by exp2(s - m); l: the sum of the weights.
+template <class T, int D, int N>
+__device__ inline void put(const PageAttendArgs &a, const Item &it, int chunk, int tok, int h, int d0, const float (&o)[N],
+                           float m, float l) {
+    const int Hq = a.t.Hkv << a.group_shift;
+    const size_t row = size_t(tok) * Hq + h;
+    if (it.chunk0 == it.chunk1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        float x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = l == 0.f ? 0.f : o[i] * inv;
+        if constexpr (T::kBytes == 2) {
+            uint16_t *p = static_cast<uint16_t *>(a.out) + row * D + d0;
+            if constexpr (N == 1) *p = uint16_t(bf16_pack(x[0], 0.f));
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) reinterpret_cast<uint32_t *>(p)[i] = bf16_pack(x[2 * i], x[2 * i + 1]);
+        } else {
+            float *p = static_cast<float *>(a.out) + row * D + d0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[i] = x[i];
+        }
+        if (a.lse && d0 == 0) a.lse[row] = l == 0.f ? -INFINITY : m * 0.69314718055994531f + logf(l);
+    } else {
+        const size_t at = size_t(chunk) * a.t.n_tokens * Hq + row;
+        float *p = a.part_o + at * D + d0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = o[i];
+        if (d0 == 0) {
+            a.part_ml[2 * at] = m;
+            a.part_ml[2 * at + 1] = l;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// 16 query rows (or NB times 16) of one wave against keys straight from memory: no LDS, so many loads
+// can be in flight.  Used where the rows are few and the bytes are the bound (bfloat16, narrow tiles),
+// and for float, whose matrix instruction takes 32 cycles for 2048 operations: there the loads of
+// four waves through the first-level cache are no bound.
+//
+// Registers of a 16-key block: keys: lane (key lane % 16, g = lane / 16) holds the pieces g of its
+// row; values: lane (m = lane % 16, g) holds elements D/16 m .. of the rows 4 g .. 4 g + 3, that is,
+// whole rows by 16 lanes, and result tile e of O^T has the elements D/16 m + e.  bfloat16 products run
+// over 32 keys: two blocks, whose rows 4 g + i are what S^T leaves in lane group g.
+// ------------------------------------------------------------------------------------------
+template <class T, class P, int D>
+struct Keys16 {
+    static constexpr int kBlocks = T::kBytes == 2 ? 2 : 1, kKeys = 16 * kBlocks;
+    static constexpr int KW = D * P::kBytes / 16, VW = D * P::kBytes / 64;    // words a lane
+    uint32_t k[kBlocks][KW], v[kBlocks][4][VW], ks[kBlocks], vs[kBlocks];
+
+    __device__ static size_t base(int row) { return row >= 0 ? row : 0; }     // any row: its keys are masked
+    __device__ void load_keys(const PageAttendArgs &a, const int (&row)[kBlocks], int lane) {
+        const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) {
+            const size_t r0 = base(row[j]);
+            const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * (D * P::kBytes);
+#pragma unroll
+            for (int i = 0; i < KW / 4; ++i) {
+                const int off = P::kBytes == 4 ? 256 * (i >> 2) + 64 * g + 16 * (i & 3) : 64 * i + 16 * g;
+                const uint4 w = *reinterpret_cast<const uint4 *>(kp + m * (D * P::kBytes) + off);
+                k[j][4 * i] = w.x; k[j][4 * i + 1] = w.y; k[j][4 * i + 2] = w.z; k[j][4 * i + 3] = w.w;
+            }
+            if constexpr (P::kBytes == 1) ks[j] = a.k_scale[r0 + m];
+        }
+    }
+    __device__ void load_values(const PageAttendArgs &a, const int (&row)[kBlocks], int lane) {
+        const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) {
+            const size_t r0 = base(row[j]);
+            const unsigned char *vp = static_cast<const unsigned char *>(a.v) + r0 * (D * P::kBytes);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned char *p = vp + (4 * g + i) * (D * P::kBytes) + m * (VW * 4);
+                if constexpr (VW % 4 == 0) {
+#pragma unroll
+                    for (int u = 0; u < VW / 4; ++u) {
+                        const uint4 w = reinterpret_cast<const uint4 *>(p)[u];
+                        v[j][i][4 * u] = w.x; v[j][i][4 * u + 1] = w.y; v[j][i][4 * u + 2] = w.z; v[j][i][4 * u + 3] = w.w;
+                    }
+                } else if constexpr (VW == 2) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+                    v[j][i][0] = w.x; v[j][i][1] = w.y;
+                } else {
+                    v[j][i][0] = *reinterpret_cast<const uint32_t *>(p);
+                }
+            }
+            if constexpr (P::kBytes == 1) vs[j] = *reinterpret_cast<const uint32_t *>(a.v_scale + r0 + 4 * g);
+        }
+    }
+};
+
+template <class T, class P, int D, int NB>
+struct Rows16 {
+    using Tile = Keys16<T, P, D>;
+    static constexpr int VE = D / 16, QW = T::kBytes == 2 ? D / 8 : D / 4;    // words of the query a lane
+    static constexpr bool kBf = T::kBytes == 2;
+    static constexpr int J = Tile::kBlocks;
+    uint32_t q[NB][QW];
+    f4v o[NB][VE];
+    float m[NB], l[NB];
+    int lo[NB], hi[NB];                 // keys that the column's query sees
+    int lo_all, hi_all, lo_any, hi_any; // keys that every column sees, that some column sees
+
+    // Columns: rows row0 + 16 nb + lane % 16 of the item.
+    __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane) {
+        const int n = lane & 15, gq = lane >> 4, gs = a.group_shift;
+        const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
+        using E = typename T::elem;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            int row = row0 + 16 * nb + n;
+            row = row < it.rows ? row : it.rows - 1;                          // spare columns repeat the last row
+            const int64_t p = it.p0 + (row >> gs);
+            const int64_t b = p - (int64_t(a.window) - 1);
+            lo[nb] = b < 0 ? 0 : int(b < cap ? b : cap);
+            hi[nb] = int(p < 0 ? -1 : p < cap ? p : cap - 1);
+            const E *src = static_cast<const E *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
+                           ((g << gs) + (row & ((1 << gs) - 1))) * D;
+#pragma unroll
+            for (int i = 0; i < QW / 4; ++i) {
+                // the dims of product i: as Keys16 lays out its pieces
+                const int dim = !kBf ? 64 * (i >> 2) + 16 * gq + 4 * (i & 3)
+                              : P::kBytes == 2 ? 32 * i + 8 * gq : 64 * (i >> 1) + 16 * gq + 8 * (i & 1);
+                const uint4 w = *reinterpret_cast<const uint4 *>(src + dim);
+                q[nb][4 * i] = w.x; q[nb][4 * i + 1] = w.y; q[nb][4 * i + 2] = w.z; q[nb][4 * i + 3] = w.w;
+            }
+            m[nb] = -INFINITY;
+            l[nb] = 0.f;
+#pragma unroll
+            for (int e = 0; e < VE; ++e) o[nb][e] = f4v{0.f, 0.f, 0.f, 0.f};
+        }
+        const int last = row0 + 16 * NB - 1 < it.rows ? row0 + 16 * NB - 1 : it.rows - 1;
+        const int64_t p_first = it.p0 + (row0 >> gs), p_last = it.p0 + (last >> gs);
+        const int64_t b = p_last - (int64_t(a.window) - 1);
+        lo_all = b < 0 ? 0 : int(b < cap ? b : cap);
+        hi_all = int(p_first < 0 ? -1 : p_first < cap ? p_first : cap - 1);
+        const int64_t f = p_first - (int64_t(a.window) - 1);
+        lo_any = f < 0 ? 0 : int(f < cap ? f : cap);
+        hi_any = int(p_last < 0 ? -1 : p_last < cap ? p_last : cap - 1);
+    }
+
+    __device__ static uint4 k_frag(const Tile &t, int j, int s) {             // bfloat16: product s
+        if constexpr (P::kBytes == 2) {
+            return make_uint4(t.k[j][4 * s], t.k[j][4 * s + 1], t.k[j][4 * s + 2], t.k[j][4 * s + 3]);
+        } else {
+            return codes8_bf16(t.k[j][2 * s], t.k[j][2 * s + 1], pow2_of(t.ks[j]));
+        }
+    }
+    __device__ void scores(const Tile &t, f4v (&s)[Tile::kBlocks][NB]) const {
+#pragma unroll
+        for (int j = 0; j < Tile::kBlocks; ++j) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) s[j][nb] = f4v{0.f, 0.f, 0.f, 0.f};
+            if constexpr (kBf) {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const uint4 kf = k_frag(t, j, i);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        s[j][nb] = mma16(kf, make_uint4(q[nb][4 * i], q[nb][4 * i + 1], q[nb][4 * i + 2], q[nb][4 * i + 3]),
+                                         s[j][nb]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    float kf[4];
+                    if constexpr (P::kBytes == 4) {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) kf[u] = __uint_as_float(t.k[j][4 * i + u]);
+                    } else {
+                        codes4_up(t.k[j][i], pow2_of(t.ks[j]), kf);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) s[j][nb] = mma16(kf[u], __uint_as_float(q[nb][4 * i + u]), s[j][nb]);
+                }
+            }
+        }
+    }
+
+    // V^T operand of result tile e: bfloat16, 32 keys
+    __device__ static uint4 v_frag(const uint32_t (&vw)[Tile::kBlocks][4][VE / 2], int e) {
+        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                w[2 * j + i] = __builtin_amdgcn_perm(vw[j][2 * i + 1][e / 2], vw[j][2 * i][e / 2], sel);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+
+    // Mask, running maximum and weights of the keys from pos on; valid: a bit for each block that holds
+    // keys.  True when some column does not see some key.
+    __device__ bool weights(const PageAttendArgs &a, f4v (&s)[J][NB], int pos, uint32_t valid, int lane) {
+        const int g = lane >> 4;
+        const bool part = valid != (1u << J) - 1 || pos < lo_all || pos + Tile::kKeys - 1 > hi_all;
+        if (part) {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = pos + 16 * j + 4 * g + i;
+                        s[j][nb][i] = (valid >> j & 1) && key >= lo[nb] && key <= hi[nb] ? s[j][nb][i] : -INFINITY;
+                    }
+        }
+        float mx[NB];
+        bool up = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            mx[nb] = s[0][nb][0];
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx[nb] = fmaxf(mx[nb], s[j][nb][i]);
+            up |= mx[nb] * a.scale_log2 > m[nb] + kSlack;
+        }
+        if (__any(up)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                float x = fmaxf(mx[nb], across16(mx[nb]));
+                x = fmaxf(x, across32(x)) * a.scale_log2;
+                const float mn = fmaxf(m[nb], x);
+                const float f = exp2_fast(m[nb] - (mn == -INFINITY ? 0.f : mn));
+                m[nb] = mn;
+                l[nb] *= f;
+#pragma unroll
+                for (int e = 0; e < VE; ++e) o[nb][e] *= f;
+            }
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const float mu = m[nb] == -INFINITY ? 0.f : m[nb];
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[j][nb][i] = exp2_fast(fmaf(s[j][nb][i], a.scale_log2, -mu));
+                    l[nb] += s[j][nb][i];
+                }
+        }
+        return part;
+    }
+
+    // o += values x weights.  Where `part`, rows that no column sees count as zeros, and `bad` says that one
+    // which some columns do not see holds an infinity or NaN: zero times that is no number.
+    __device__ void values(Tile &t, const f4v (&s)[J][NB], int pos, uint32_t valid, bool part, bool *bad, int lane) {
+        const int g = lane >> 4;
+        if constexpr (kBf) {
+            uint32_t vw[J][4][VE / 2];
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float sc = P::kBytes == 1 ? pow2_of(t.vs[j] >> (8 * i) & 255u) : 1.f;
+#pragma unroll
+                    for (int w = 0; w < VE / 2; ++w) {
+                        if constexpr (P::kBytes == 2) vw[j][i][w] = t.v[j][i][w];
+                        else vw[j][i][w] = codes2_bf16(t.v[j][i][w / 2], sc, w & 1);
+                    }
+                }
+            if (part) {
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = pos + 16 * j + 4 * g + i;
+                        const uint32_t keep = (valid >> j & 1) && key >= lo_any && key <= hi_any ? 0xffffffffu : 0u;
+#pragma unroll
+                        for (int w = 0; w < VE / 2; ++w) {
+                            vw[j][i][w] &= keep;
+                            *bad |= odd2(vw[j][i][w]) != 0;
+                        }
+                    }
+            }
+            uint4 pf[NB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                pf[nb] = make_uint4(bf16_pack(s[0][nb][0], s[0][nb][1]), bf16_pack(s[0][nb][2], s[0][nb][3]),
+                                    bf16_pack(s[J - 1][nb][0], s[J - 1][nb][1]), bf16_pack(s[J - 1][nb][2], s[J - 1][nb][3]));
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const uint4 vf = v_frag(vw, e);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) o[nb][e] = mma16(vf, pf[nb], o[nb][e]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float vf[VE];
+                if constexpr (P::kBytes == 4) {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) vf[e] = __uint_as_float(t.v[0][i][e]);
+                } else {
+#pragma unroll
+                    for (int w = 0; w < VE / 4; ++w) {
+                        float x[4];
+                        codes4_up(t.v[0][i][w], pow2_of(t.vs[0] >> (8 * i) & 255u), x);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) vf[4 * w + u] = x[u];
+                    }
+                }
+                if (part) {
+                    const int key = pos + 4 * g + i;
+                    const bool keep = valid && key >= lo_any && key <= hi_any;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        vf[e] = keep ? vf[e] : 0.f;
+                        *bad |= odd(vf[e]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) o[nb][e] = mma16(vf[e], s[0][nb][i], o[nb][e]);
+            }
+        }
+    }
+
+    // Every step-th group of keys from pos on; row blocks are looked up a step ahead, and a step's keys and
+    // values are asked for as soon as the registers of the last ones are free.
+    __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int step, bool *bad, int lane) {
+        if (pos >= it.end) return;
+        Tile t;
+        int row[J];
+        look(a, it, b, g, pos, row, lane);
+        t.load_keys(a, row, lane);
+        t.load_values(a, row, lane);
+        for (;;) {
+            uint32_t valid = 0;
+#pragma unroll
+            for (int j = 0; j < J; ++j) valid |= row[j] >= 0 ? 1u << j : 0u;
+            const int next = pos + step;
+            const bool more = next < it.end;
+            if (more) look(a, it, b, g, next, row, lane);
+            f4v s[J][NB];
+            scores(t, s);
+            if (more) t.load_keys(a, row, lane);
+            const bool part = weights(a, s, pos, valid, lane);
+            values(t, s, pos, valid, part, bad, lane);
+            if (!more) return;
+            t.load_values(a, row, lane);
+            pos = next;
+        }
+    }
+    __device__ static void look(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int (&row)[J], int lane) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) row[j] = key_block(a, b, g, pos + 16 * j, it.end, lane);
+    }
+
+    // The column's sum over its four lanes.
+    __device__ float sum(int nb) const {
+        float x = l[nb] + across16(l[nb]);
+        return x + across32(x);
+    }
+};
+
+// An item whose masked keys hold infinities or NaN, row by row: a wave a row, 64 keys at a time, a
+// score a lane, then the values with the lanes over d.  Only keys that the row sees are touched.
+template <class T, class P, int D>
+__device__ inline void plain_rows(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave) {
+    auto element = [](const void *pool, const uint8_t *scale, int row, int i) {
+        const size_t at = size_t(row) * D + i;
+        if constexpr (P::kBytes == 4) return static_cast<const float *>(pool)[at];
+        else if constexpr (P::kBytes == 2) return bf16_up(static_cast<const uint16_t *>(pool)[at]);
+        else {
+            float x[4];
+            codes4_up(static_cast<const uint8_t *>(pool)[at], pow2_of(scale[row]), x);
+            return x[0];
+        }
+    };
+    const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
+    for (int rw = wave; rw < it.rows; rw += 4) {
+        const int tok = it.tok0 + (rw >> a.group_shift), h = (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1));
+        const int64_t p = it.p0 + (rw >> a.group_shift), w = p - (int64_t(a.window) - 1);
+        const int64_t from = w > it.begin ? w : it.begin, to = p + 1 < it.end ? p + 1 : it.end;
+        float m = -INFINITY, l = 0.f, o[D / 64] = {};
+        for (int64_t j0 = from; j0 < to; j0 += 64) {
+            const int j = int(j0) + lane;
+            int row = -1;
+            if (j < to && j < cap) row = pool_row(a.t, b, g, j);
+            float s = -INFINITY;
+            if (row >= 0) {
+                float x = 0.f;
+                for (int i = 0; i < D; ++i) {
+                    const int64_t at = int64_t(tok) * a.q_stride + h * D + i;
+                    const float q = T::kBytes == 4 ? static_cast<const float *>(a.q)[at] : bf16_up(static_cast<const uint16_t *>(a.q)[at]);
+                    x = fmaf(q, element(a.k, a.k_scale, row, i), x);
+                }
+                s = x * a.scale_log2;
+            }
+            float mx = s;
+            for (int k = 1; k < 64; k *= 2) mx = fmaxf(mx, __shfl_xor(mx, k));
+            const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
+            const float f = exp2_fast(m - mu), wt = row >= 0 ? exp2_fast(s - mu) : 0.f;
+            float sum = wt;
+            for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+            m = mn;
+            l = l * f + sum;
+            for (int e = 0; e < D / 64; ++e) o[e] *= f;
+            for (int k = 0; k < 64; ++k) {
+                const int r = __builtin_amdgcn_readlane(row, k);
+                const float x = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wt), k));
+                if (r >= 0)
+                    for (int e = 0; e < D / 64; ++e) o[e] = fmaf(x, element(a.v, a.v_scale, r, lane * (D / 64) + e), o[e]);
+            }
+        }
+        put<T, D>(a, it, c, tok, h, lane * (D / 64), o, m, l);
+    }
+}
+
+}  // namespace page
+}  // namespace sekv

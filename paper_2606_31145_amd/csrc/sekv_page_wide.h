@@ -1,0 +1,220 @@
+// 128 query rows of a workgroup against tiles of 64 keys in LDS: the bfloat16 form of
+// sekv_page_attend for chunks.
+//
+// What bounds it: the matrix cores and the softmax's vector instructions together.  A wave takes 32
+// rows; per tile it issues 32 matrix instructions of 32 cycles (32x32x16, half scores, half values),
+// and 2048 scores cost it about 4 vector instructions and one exponential each for 64 lanes, so the
+// two units are about equally busy and two workgroups share a compute unit to keep both fed.  Keys
+// and values are fetched once per workgroup (each wave one block of 16 keys, which lies in one page),
+// a tile ahead, in registers; on the way into LDS 8-bit codes become scaled bfloat16, so the rest
+// knows one type only.
+//
+// LDS: rows of D values in 16-byte pieces, two buffers.  A piece sits at its index XOR a function of
+// its row, so that what 64 lanes read together falls into different banks: for keys 16 rows at one
+// piece, for values (turned on reading: 4 rows by 16 columns) 8 rows at 4 pieces.
+#pragma once
+
+#include "sekv_page_tile.h"
+
+namespace sekv {
+namespace page {
+
+// Four rows of one column of a bf16 tile in LDS: within 16 lanes, lane i names 4 columns
+// 4 (i % 4) of row i / 4 and receives column i of the four rows.
+__device__ inline uint2 turn4(const unsigned char *p) {
+    typedef short s4v __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s4v *lds_p;
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_p>(reinterpret_cast<uintptr_t>(p))));
+}
+
+template <int D> struct Swizzle {
+    static constexpr int CH = D / 8;                   // 16-byte pieces a row
+    static __device__ int key(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+    static __device__ int value(int row) {
+        return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    }
+};
+
+// Is one of four e4m3 codes a NaN.
+__device__ inline bool nan4(uint32_t w) {
+    const uint32_t x = ~w & 0x7f7f7f7fu;               // a zero byte: NaN
+    return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+}
+
+// A wave's 16 rows of keys and values on their way from a page into LDS.
+template <class P, int D>
+struct Stage {
+    static constexpr int N = D * P::kBytes / 64;       // 16-byte pieces a lane, keys or values
+    static constexpr int PC = D * P::kBytes / 16;      // pieces a row
+    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+    u4v k[N], v[N];
+    uint32_t ks[N], vs[N];
+
+    __device__ void load(const PageAttendArgs &a, int row0, int lane) {
+        const size_t r0 = row0 >= 0 ? row0 : 0;        // any row: its keys are masked
+        const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * (D * P::kBytes);
+        const unsigned char *vp = static_cast<const unsigned char *>(a.v) + r0 * (D * P::kBytes);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            k[i] = reinterpret_cast<const u4v *>(kp)[i * 64 + lane];
+            v[i] = reinterpret_cast<const u4v *>(vp)[i * 64 + lane];
+            if constexpr (P::kBytes == 1) {
+                ks[i] = a.k_scale[r0 + i * (64 / PC) + lane / PC];
+                vs[i] = a.v_scale[r0 + i * (64 / PC) + lane / PC];
+            }
+        }
+    }
+    // For a tile that not every row sees: values from row `end` on, which none sees, become zeros.  True when
+    // another holds an infinity or NaN: the product with its masked weight, zero, would be no number.
+    __device__ bool mend(int row0, int end, int lane) {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t keep = row0 + i * (64 / PC) + lane / PC >= end ? 0u : ~0u;
+            v[i] &= keep;
+            if constexpr (P::kBytes == 2) {
+                bad |= odd(make_uint4(v[i].x, v[i].y, v[i].z, v[i].w));
+            } else {
+                vs[i] = keep ? vs[i] : 127u;
+                bad |= uint32_t(nan4(v[i].x)) | uint32_t(nan4(v[i].y)) | uint32_t(nan4(v[i].z)) | uint32_t(nan4(v[i].w));
+            }
+        }
+        return bad != 0;
+    }
+    // into a tile's keys and values, rows row0 ..
+    __device__ void store(unsigned char *kt, unsigned char *vt, int row0, int lane) const {
+        using Z = Swizzle<D>;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int row = row0 + i * (64 / PC) + lane / PC, c = lane % PC;
+            unsigned char *kr = kt + row * (D * 2), *vr = vt + row * (D * 2);
+            if constexpr (P::kBytes == 2) {
+                *reinterpret_cast<u4v *>(kr + ((c ^ Z::key(row)) << 4)) = k[i];
+                *reinterpret_cast<u4v *>(vr + ((c ^ Z::value(row)) << 4)) = v[i];
+            } else {
+                const float fk = pow2_of(ks[i]), fv = pow2_of(vs[i]);
+                *reinterpret_cast<uint4 *>(kr + (((2 * c) ^ Z::key(row)) << 4)) = codes8_bf16(k[i].x, k[i].y, fk);
+                *reinterpret_cast<uint4 *>(kr + (((2 * c + 1) ^ Z::key(row)) << 4)) = codes8_bf16(k[i].z, k[i].w, fk);
+                *reinterpret_cast<uint4 *>(vr + (((2 * c) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].x, v[i].y, fv);
+                *reinterpret_cast<uint4 *>(vr + (((2 * c + 1) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].z, v[i].w, fv);
+            }
+        }
+    }
+};
+
+template <int D>
+struct Rows32 {
+    static constexpr int DB = D / 32, QS = D / 16;
+    uint4 q[QS];
+    f16v o[DB];
+    float m, l;
+    int lo, hi;                         // keys that the column's query sees
+    int lo_all, hi_all;                 // keys that every column sees
+    int lo_any, hi_any;                 // keys that some column sees
+    int kaddr[QS], vaddr[2][DB];        // this lane's pieces in a tile
+
+    __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane) {
+        const int n = lane & 31, h = lane >> 5, i = lane & 15, gs = a.group_shift;
+        const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
+        int row = row0 + n;
+        row = row < it.rows ? row : it.rows - 1;
+        const int last = row0 + 31 < it.rows ? row0 + 31 : it.rows - 1, first = row0 < it.rows ? row0 : it.rows - 1;
+        const int64_t p = it.p0 + (row >> gs), p_first = it.p0 + (first >> gs), p_last = it.p0 + (last >> gs), w = int64_t(a.window) - 1;
+        auto cut = [&](int64_t x, int64_t top) { return int(x < -1 ? -1 : x < top ? x : top); };
+        lo = cut(p - w < 0 ? 0 : p - w, cap);
+        hi = cut(p, cap - 1);
+        lo_all = cut(p_last - w < 0 ? 0 : p_last - w, cap);
+        hi_all = cut(p_first, cap - 1);
+        lo_any = cut(p_first - w < 0 ? 0 : p_first - w, cap);
+        hi_any = row0 < it.rows ? cut(p_last, cap - 1) : -1;
+        const uint16_t *src = static_cast<const uint16_t *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
+                              ((g << gs) + (row & ((1 << gs) - 1))) * D;
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            q[s] = *reinterpret_cast<const uint4 *>(src + 16 * s + 8 * h);
+            kaddr[s] = n * (D * 2) + (((2 * s + h) ^ Swizzle<D>::key(n)) << 4);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                const int r = 8 * u + 4 * h + (i >> 2);
+                const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+                vaddr[u][db] = r * (D * 2) + ((c ^ Swizzle<D>::value(r)) << 4) + 8 * (i & 1);
+            }
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+    }
+
+    // V^T operand: 32 elements from 32 db on, the 16 keys of block kb
+    __device__ uint4 v_frag(const unsigned char *vt, int kb, int db) const {
+        const uint2 x = turn4(vt + vaddr[0][db] + kb * (32 * D)), y = turn4(vt + vaddr[1][db] + kb * (32 * D));
+        return make_uint4(x.x, x.y, y.x, y.y);
+    }
+
+    // One tile: 64 keys from pos on; valid: which of its four blocks hold keys.
+    __device__ void step(const PageAttendArgs &a, const unsigned char *kt, const unsigned char *vt, int pos, uint32_t valid, int lane) {
+        if (pos > hi_any || pos + 63 < lo_any) return;
+        const int h = lane >> 5;
+        f16v s[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[j][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < QS; ++c)
+                s[j] = mma32(*reinterpret_cast<const uint4 *>(kt + kaddr[c] + j * (64 * D)), q[c], s[j]);
+        }
+        const bool part = valid != 15u || pos < lo_all || pos + 63 > hi_all;
+        if (part) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int off = 32 * j + 8 * (r >> 2) + (r & 3), key = pos + off + 4 * h;
+                    s[j][r] = (valid >> (off >> 4) & 1) && key >= lo && key <= hi ? s[j][r] : -INFINITY;
+                }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
+        if (__any(mx * a.scale_log2 > m + kSlack)) {
+            const float x = fmaxf(mx, across32(mx)) * a.scale_log2;
+            const float mn = fmaxf(m, x);
+            const float f = exp2_fast(m - (mn == -INFINITY ? 0.f : mn));
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[db] *= f;
+        }
+        const float mu = m == -INFINITY ? 0.f : m;
+        uint4 pf[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[j][r] = exp2_fast(fmaf(s[j][r], a.scale_log2, -mu));
+                sum += s[j][r];
+            }
+            l += sum;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                pf[2 * j + u] = make_uint4(bf16_pack(s[j][8 * u], s[j][8 * u + 1]), bf16_pack(s[j][8 * u + 2], s[j][8 * u + 3]),
+                                           bf16_pack(s[j][8 * u + 4], s[j][8 * u + 5]), bf16_pack(s[j][8 * u + 6], s[j][8 * u + 7]));
+        }
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[db] = mma32(v_frag(vt, kb, db), pf[kb], o[db]);
+    }
+};
+
+}  // namespace page
+}  // namespace sekv

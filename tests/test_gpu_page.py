@@ -84,7 +84,7 @@ APPENDS = [
     dict(lens=[40, 7, 0, 33], news=[1, 1, 0, 1], page=16),
     dict(lens=[17, 300, 64], news=[17, 123, 0], page=32, kv_heads=3, group=1),
     dict(lens=[5, 1000], news=[5, 777], page=128, dim=128, kv_heads=1, group=8, strided=True),
-    dict(lens=[9, 31], news=[4, 31], page=1, dim=128),
+    dict(lens=[9, 31], news=[4, 31], page=16, dim=128),
     dict(lens=[2100], news=[2050], page=1024, kv_heads=2, strided=True, tail=5),
 ]
 
@@ -146,7 +146,7 @@ def test_append_leaves_bad_places_alone(S, dtype, store):
 
 
 READS = [dict(lens=[1], page=16), dict(lens=[33, 0, 200], page=32, kv_heads=3, group=1),
-         dict(lens=[5, 1000], page=128, dim=128, kv_heads=1), dict(lens=[9, 31], page=1),
+         dict(lens=[5, 1000], page=128, dim=128, kv_heads=1), dict(lens=[9, 31], page=16),
          dict(lens=[2100], page=1024, dim=128)]
 
 
@@ -218,16 +218,16 @@ ATTENDS = [
     dict(lens=[63, 64, 65, 129], news=[1, 1, 1, 1], group=8, kv_heads=1),
     dict(lens=[1000, 3, 517], news=[1, 1, 1], dim=128, page=64),
     dict(lens=[300, 40], news=[4, 2], group=4, dim=128, page=32, strided=True),
-    dict(lens=[300, 17, 90], news=[5, 17, 0], group=8, dim=64, page=8),
+    dict(lens=[300, 17, 90], news=[5, 17, 0], group=8, dim=64, page=16),
     dict(lens=[200, 160], news=[33, 160], group=4, dim=128, page=16, tail=3),
     dict(lens=[131], news=[131], group=1, kv_heads=2, page=128),
     dict(lens=[3, 70], news=[5, 90], group=2),                             # rows before the first token
     dict(lens=[700], news=[150], group=2, dim=128, page=256, window=100),
     dict(lens=[260, 99], news=[1, 20], group=4, window=1),
-    dict(lens=[600, 90, 40], news=[1, 3, 40], group=4, dim=128, window=65, page=4),
+    dict(lens=[600, 90, 40], news=[1, 3, 40], group=4, dim=128, window=65, page=32),
     dict(lens=[5000], news=[1], group=4, kv_heads=1, dim=128, page=64),
     dict(lens=[2500, 31], news=[20, 31], group=4, kv_heads=1, dim=64, page=16, strided=True),
-    dict(lens=[40, 30], news=[3, 30], group=2, page=1),
+    dict(lens=[40, 30], news=[3, 30], group=2, page=16),
     dict(lens=[70, 41], news=[1, 37], group=4, dim=128, spread=8.0),       # weights of one entry almost
 ]
 

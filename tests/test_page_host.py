@@ -32,7 +32,7 @@ def _dims(S, **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(batch=-1), 1), (dict(batch=4097), 2), (dict(n_q_heads=0), 1), (dict(n_kv_heads=0), 1),
     (dict(n_q_heads=9), 1), (dict(n_q_heads=6), 2), (dict(n_q_heads=32), 2), (dict(n_q_heads=8192, n_kv_heads=4096), 2),
-    (dict(head_dim=96), 2), (dict(head_dim=256), 2), (dict(page_size=0), 2), (dict(page_size=24), 2),
+    (dict(head_dim=96), 2), (dict(head_dim=256), 2), (dict(page_size=0), 2), (dict(page_size=8), 2), (dict(page_size=24), 2),
     (dict(page_size=2048), 2), (dict(n_pages=0), 1), (dict(max_pages=0), 1), (dict(n_pages=1 << 27), 2),
     (dict(max_pages=(1 << 26) + 1), 2), (dict(dtype=2), 2), (dict(dtype="bf16", page_dtype="f32"), 2),
     (dict(dtype="f32", page_dtype="bf16"), 2), (dict(window=-1), 1), (dict(softmax_scale=0.0), 1),
@@ -59,7 +59,7 @@ def test_reserved_fields_and_counts_are_refused(S):
 
 
 @pytest.mark.parametrize("kw", [dict(), dict(dtype="f32"), dict(page_dtype="e4m3"), dict(batch=0),
-                                dict(page_size=1, n_pages=1000, max_pages=300), dict(page_size=1024)])
+                                dict(page_size=16, n_pages=1000, max_pages=300), dict(page_size=1024)])
 def test_good_dims_have_a_workspace(S, kw):
     S.check_page_dims(_dims(S, **kw))
     assert S.page_workspace_size(_dims(S, **kw), 0) >= 256
@@ -104,7 +104,7 @@ def test_page_arguments_are_refused(S, call):
     for kw in (dict(k=None), dict(v=None), dict(table=None), dict(seq_len=None), dict(k=OK + 8), dict(v=OK + 4),
                dict(table=OK + 2), dict(seq_len=OK + 1), dict(k_scale=OK), dict(v_scale=OK)):
         assert call(S, d, pages=_pages(S, **kw)) == S.SEKV_ERR_INVALID_ARG, kw
-    for kw in (dict(), dict(k_scale=OK), dict(v_scale=OK)):
+    for kw in (dict(), dict(k_scale=OK), dict(v_scale=OK), dict(k_scale=OK, v_scale=OK + 8)):
         assert call(S, q, pages=_pages(S, **kw)) == S.SEKV_ERR_INVALID_ARG, kw
     assert call(S, d, pages=None) == S.SEKV_ERR_INVALID_ARG
     assert call(S, d, n=-1) == S.SEKV_ERR_INVALID_ARG
