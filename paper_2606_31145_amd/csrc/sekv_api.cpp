@@ -16,6 +16,7 @@
 #include "sekv.h"
 #include "sekv_host.h"
 #include "sekv_internal.h"
+#include "sekv_page_internal.h"
 
 namespace {
 
@@ -180,10 +181,12 @@ void ws_note_zeroed(void *ws, size_t bytes) {
 
 }  // namespace
 namespace sekv {
-// A call with no layout of its own state has written over a workspace: the next step zeroes it.
-void note_foreign_use(void *ws, size_t bytes) {
+hipError_t ws_prepare_pages(void *ws, size_t bytes, size_t words, hipStream_t stream) {
     std::lock_guard<std::mutex> lk(g_ws_mu);
-    (void)g_ws.before_launch(reinterpret_cast<uintptr_t>(ws), bytes, ~uint64_t(0), 1);
+    // the counters are all that has to be zero, and their number is all that their place depends on
+    if (g_ws.before_launch(reinterpret_cast<uintptr_t>(ws), bytes, (uint64_t(0x5047) << 48) | words, 1))
+        return launch_zero_words(static_cast<unsigned char *>(ws) + sizeof(WsHeader), words, stream);
+    return hipSuccess;
 }
 }  // namespace sekv
 namespace {

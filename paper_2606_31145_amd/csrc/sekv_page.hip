@@ -154,6 +154,10 @@ __global__ void __launch_bounds__(kThreads) read_kernel(PageReadArgs a) {
     }
 }
 
+__global__ void __launch_bounds__(kThreads) zero_words_kernel(uint32_t *p, size_t n) {
+    for (size_t i = size_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += size_t(gridDim.x) * kThreads) p[i] = 0;
+}
+
 template <class T, class P, int D>
 hipError_t append(const PageAppendArgs &a, hipStream_t s) {
     constexpr int kRows = kThreads / (D / Piece<T>::kN);
@@ -183,6 +187,13 @@ hipError_t dispatch(int dtype, int page_dtype, int d, F f) {
 }
 
 }  // namespace
+
+hipError_t launch_zero_words(void *p, size_t words, hipStream_t stream) {
+    const size_t blocks = (words + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(zero_words_kernel, dim3(unsigned(blocks < 1024 ? blocks : 1024)), dim3(kThreads), 0, stream,
+                       static_cast<uint32_t *>(p), words);
+    return hipGetLastError();
+}
 
 hipError_t launch_page_append(const PageAppendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream) {
     return dispatch(dtype, page_dtype, head_dim, [&](auto t, auto p, auto d) { return append<decltype(t), decltype(p), decltype(d)::value>(a, stream); });

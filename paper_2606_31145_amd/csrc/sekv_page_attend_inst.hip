@@ -170,22 +170,34 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
     const int g = blockIdx.x % a.t.Hkv, chunk = find_chunk(a, lane);
     int b = 0, c = 0;
     Item it;
-    if (!find_item(a, blockIdx.x / a.t.Hkv, lane, chunk, &b, &c, &it)) return;
+    if (!chunk || !find_item(a, blockIdx.x / a.t.Hkv, lane, chunk, &b, &c, &it)) return;
     bool again;
     if (it.narrow) again = narrow<T, P, D>(a, it, b, g, c, lane, wave, lds);
     else if constexpr (T::kBytes == 2) again = wide_bf16<P, D>(a, it, b, g, c, lane, wave, lds);
     else again = wide_f32<P, D>(a, it, b, g, c, lane, wave);
     if (again) plain_rows<T, P, D>(a, it, b, g, c, lane, wave);
+    if (it.chunk0 == it.chunk1 || a.join_launch) return;
+    // the last of a tile's workgroups joins their partials: all stores of this one have to be out before it
+    // counts itself, and the last one sets the counter back
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    __shared__ uint32_t before;
+    uint32_t *cnt = a.arrived + size_t(it.tok0) * a.t.Hkv + g;
+    if (threadIdx.x == 0) before = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (before != uint32_t(it.chunk1 - it.chunk0)) return;
+    if (threadIdx.x == 0) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    join_rows<T, D, true>(a, it, g, 0, it.rows, lane, lds);
 }
 
-// Joins the partials of one token and head: one wave, the lanes over d.
+// Joins the partials of a token's query heads of one KV head.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
-    const int lane = threadIdx.x & 63, Hq = a.t.Hkv << a.group_shift;
-    const int64_t row = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-    const int tok = __builtin_amdgcn_readfirstlane(int(row / Hq)), h = int(row % Hq);
-    if (tok >= a.t.n_tokens) return;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[256 * (sizeof(float4) + sizeof(float2))];
+    const int lane = threadIdx.x & 63, tok = blockIdx.x / a.t.Hkv, g = blockIdx.x % a.t.Hkv;
     const int chunk = find_chunk(a, lane);
+    if (!chunk) return;
     int lo = 0, hi = a.t.B;                                  // the last b with tok_start[b] <= tok
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -195,21 +207,9 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
     if (tok < s.start || tok >= s.start + s.nq) return;
     const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
     const int tile = (s.nq << a.group_shift) <= kNarrowRows ? 0 : ((tok - s.start) << a.group_shift) / kTileRows;
-    Item it = make_item(s, tile, 0, chunk, cap, a.window, a.group_shift);
+    const Item it = make_item(s, tile, 0, chunk, cap, a.window, a.group_shift);
     if (it.chunk0 == it.chunk1) return;
-    float m = -INFINITY, l = 0.f, o[D / 64] = {};
-    const size_t step = size_t(a.t.n_tokens) * Hq, at0 = size_t(tok) * Hq + h;
-    for (int c = it.chunk0; c <= it.chunk1; ++c) m = fmaxf(m, a.part_ml[2 * (c * step + at0)]);
-    const float mu = m == -INFINITY ? 0.f : m;
-    for (int c = it.chunk0; c <= it.chunk1; ++c) {
-        const size_t at = c * step + at0;
-        const float f = exp2_fast(a.part_ml[2 * at] - mu);
-        l += f * a.part_ml[2 * at + 1];
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) o[i] += f * a.part_o[at * D + lane * (D / 64) + i];
-    }
-    it.chunk0 = it.chunk1;
-    put<T, D>(a, it, 0, tok, h, lane * (D / 64), o, m, l);
+    join_rows<T, D, false>(a, it, g, (tok - it.tok0) << a.group_shift, 1 << a.group_shift, lane, lds);
 }
 
 }  // namespace
@@ -222,9 +222,8 @@ hipError_t SEKV_NAME(SEKV_T, SEKV_P, SEKV_D)(const PageAttendArgs &a, hipStream_
     using P = page::SEKV_P;
     hipLaunchKernelGGL((attend_kernel<T, P, SEKV_D>), dim3(unsigned(a.pairs * a.t.Hkv)), dim3(kThreads), 0, s, a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t rows = int64_t(a.t.n_tokens) * (a.t.Hkv << a.group_shift);
-    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
+    if (e != hipSuccess || a.splits == 1 || !a.join_launch) return e;
+    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned(a.t.n_tokens) * unsigned(a.t.Hkv)), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 

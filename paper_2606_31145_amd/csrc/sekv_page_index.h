@@ -5,11 +5,19 @@
 // into tiles of kTileRows, or are one narrow tile when there are at most kNarrowRows.  A tile's keys
 // are cut into chunks so that few rows over many keys still fill the device.  The chunk length is
 // found from the device's tables, the same for the whole call: with T_b tiles and L_b keys of
-// sequence b, W = sum T_b L_b, chunk = max(W / target, max L_b / splits) in steps of kChunkStep
+// sequence b, W = sum T_b L_b, chunk >= max(W / target, max L_b / splits) in steps of kChunkStep
 // keys.  Then there are at most sum T_b + target (tile, chunk) pairs, whatever the lengths: the grid
 // can be sized before they are known, and no sequence gets more than `splits` chunks.
+//
+// Above that bound the length follows a model of the time, in keys: an item costs its keys and
+// `over` more (its start, and the join of its partial), and `slots` items run at once.  Where
+// the lengths are alike, k full rounds of items cost k (L / n + over) with n = k slots / T chunks a
+// tile; the best of a few k is taken, or no cut at all.  Where they differ, the time is at most
+// (W + (W / chunk) over) / slots + chunk, the last term being the item that ends last; that is least
+// at chunk = sqrt(W over / slots).
 #pragma once
 
+#include <math.h>
 #include <stdint.h>
 
 #ifdef __HIPCC__
@@ -23,7 +31,9 @@ namespace page {
 
 constexpr int kNarrowRows = 16;    // columns of a 16-wide matrix tile
 constexpr int kTileRows = 128;     // 32 rows for each of four waves
-constexpr int kChunkStep = 256;    // keys: a step of 64 for each of four waves
+constexpr int kChunkStep = 128;    // keys: a step of 32 for each of four waves
+constexpr int kSlots = 512;        // workgroups that run at once: two on each of 256 compute units
+constexpr int kOverNarrow = 128, kOverWide = 512;    // keys that an item costs beside its own
 constexpr int kBlock = 16;         // keys that lie in one page: the smallest page
 
 // Pool row of position `pos` (below max_pages * page_size) from its table entry; -1 when the page is
@@ -58,12 +68,30 @@ SEKV_HD Seq make_seq(int start, int end, int seq_len, int n_tokens, int64_t cap,
     return s;
 }
 
-SEKV_HD int chunk_length(uint64_t W, int max_len, int target, int splits) {
+// W, T: of one KV head
+SEKV_HD int chunk_length(uint64_t W, int T, int max_len, int Hkv, int target, int splits, int over) {
     uint64_t c = (W + target - 1) / uint64_t(target);
     const uint64_t d = (uint64_t(max_len) + splits - 1) / uint64_t(splits);
     c = c > d ? c : d;
+    const float mean = T > 0 ? float(W) / float(T) : 0.f, all = float(T) * float(Hkv);
+    float best = float(max_len);                             // no cut
+    if (float(max_len) <= 1.1f * mean) {
+        const int rounds = int((all + float(kSlots - 1)) / float(kSlots));
+        float cost = float(rounds) * mean;
+        for (int k = 1; k <= 4; ++k) {
+            const float n = float(int(float(k * kSlots) / all));
+            const float x = n > 1.f ? float(k) * (mean / n + float(over)) : cost;
+            best = x < cost ? mean / n : best;
+            cost = x < cost ? x : cost;
+        }
+    } else {
+        const float x = sqrtf(mean * all * float(over) / float(kSlots));
+        best = x < best ? x : best;
+    }
+    const uint64_t m = uint64_t(best) + 1;
+    c = c > m ? c : m;
     c = (c + kChunkStep - 1) / kChunkStep * kChunkStep;
-    return int(c < kChunkStep ? kChunkStep : c > (1u << 30) ? (1u << 30) : c);
+    return int(c > (1u << 30) ? (1u << 30) : c);
 }
 SEKV_HD int chunks_of(const Seq &s, int chunk) { return s.len > chunk ? (s.len + chunk - 1) / chunk : 1; }
 
@@ -134,6 +162,19 @@ SEKV_HD int64_t partial_rows(int n_tokens, int Hkv, int group_shift, int64_t cap
     const int64_t rows = int64_t(n_tokens) << group_shift, target = (items + Hkv - 1) / Hkv;
     const int64_t a = target * kTileRows + rows, b = rows * most_splits(cap);
     return (a < b ? a : b) * Hkv;
+}
+
+// Counters that any call of these dims needs, [n_tokens][Hkv]: only calls with splits > 1 have any, and
+// those have rows < target * kTileRows.  A number of the dims alone, so that calls of all sizes keep them
+// in the same place.
+SEKV_HD int64_t counter_words(int Hkv, int group_shift, int items) {
+    return (int64_t((items + Hkv - 1) / Hkv) * kTileRows >> group_shift) * Hkv;
+}
+// Whether the partials go to a second kernel.  Joining in the last workgroup of a tile saves a launch but
+// leaves a tile of 128 rows to one compute unit, so it is for tiles that are probably narrow; more new
+// tokens than narrow tiles hold mean that some tile is not.
+SEKV_HD bool join_in_launch(int batch, int n_tokens, int group_shift) {
+    return (int64_t(n_tokens) << group_shift) > int64_t(batch) * kNarrowRows;
 }
 
 }  // namespace page

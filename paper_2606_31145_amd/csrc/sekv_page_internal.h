@@ -56,13 +56,17 @@ struct PageAttendArgs {
     int32_t splits, target;    // see sekv_page_index.h
     int64_t pairs;
     float scale_log2;          // softmax_scale * log2(e)
+    int32_t join_launch;       // partials are joined by a second kernel, not by a tile's last workgroup
+    uint32_t *arrived;         // [n_tokens][Hkv] by a tile's first token: its chunks that are done; zero between calls
     float *part_o;             // [splits][n_tokens][Hq][d]
     float *part_ml;            // [splits][n_tokens][Hq][2]: maximum (base 2), sum
 };
 
-// sekv_api.cpp: a workspace that the step calls may share holds something else now.
-void note_foreign_use(void *ws, size_t bytes);
+// sekv_api.cpp: a page call with `words` counters behind the header is about to run on this workspace;
+// they are zeroed on the stream unless the last call there left them so.
+hipError_t ws_prepare_pages(void *ws, size_t bytes, size_t words, hipStream_t stream);
 
+hipError_t launch_zero_words(void *p, size_t words, hipStream_t stream);
 hipError_t launch_page_append(const PageAppendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);
 hipError_t launch_page_read(const PageReadArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);
 hipError_t launch_page_attend(const PageAttendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);

@@ -53,26 +53,33 @@ __device__ inline Seq load_seq(const PageAttendArgs &a, int b) {
                     a.window, a.group_shift);
 }
 
-// The call's chunk length: two sums over the batch.
+// The call's chunk length: three sums over the batch.  0 where tok_start does not ascend within the new
+// tokens: rows could then belong to two sequences, and a tile's counter to two tiles.
 __device__ inline int find_chunk(const PageAttendArgs &a, int lane) {
     if (a.splits == 1) return 1 << 30;
     uint64_t W = 0;
-    int mx = 0;
+    int mx = 0, T = 0;
+    bool wrong = false;
     for (int b = lane; b < a.t.B; b += 64) {
         const Seq s = load_seq(a, b);
+        wrong |= a.t.tok_start[b] != s.start || a.t.tok_start[b + 1] != s.start + s.nq;
         W += uint64_t(s.tiles) * uint64_t(s.len);
+        T += s.tiles;
         mx = mx > s.len ? mx : s.len;
     }
+    if (__any(wrong)) return 0;
     if (a.t.B > 1) {
 #pragma unroll
         for (int k = 1; k < 64; k *= 2) {
             W += __shfl_xor((unsigned long long)W, k);
+            T += __shfl_xor(T, k);
             const int y = __shfl_xor(mx, k);
             mx = mx > y ? mx : y;
         }
     }
     W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
-    return chunk_length(W, __builtin_amdgcn_readfirstlane(mx), a.target, a.splits);
+    return chunk_length(W, __builtin_amdgcn_readfirstlane(T), __builtin_amdgcn_readfirstlane(mx), a.t.Hkv, a.target,
+                        a.splits, a.join_launch ? kOverWide : kOverNarrow);
 }
 
 // Pair x of the call: sequences in order, chunks of a sequence in order, tiles last first (the later
@@ -121,6 +128,24 @@ __device__ inline int key_block(const PageAttendArgs &a, int b, int g, int pos, 
     return r;
 }
 
+// Partials that the last workgroup of a tile joins cross between the chip's L2 caches: written through
+// and read past them.  A second kernel sees plain stores.
+template <bool kThrough>
+__device__ inline void put_pair(float *p, float x, float y) {
+    if (!kThrough) {
+        *reinterpret_cast<float2 *>(p) = make_float2(x, y);
+        return;
+    }
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), __float_as_uint(x) | uint64_t(__float_as_uint(y)) << 32,
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool kThrough>
+__device__ inline float2 get_pair(const float *p) {
+    if (!kThrough) return *reinterpret_cast<const float2 *>(p);
+    const uint64_t w = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float(uint32_t(w)), __uint_as_float(uint32_t(w >> 32)));
+}
+
 // Where a row's result goes: the output, or a partial of its chunk.  o: N consecutive values from d0
 // on, weighted by exp2(s - m); l: the sum of the weights.
 template <class T, int D, int N>
@@ -147,11 +172,17 @@ __device__ inline void put(const PageAttendArgs &a, const Item &it, int chunk, i
     } else {
         const size_t at = size_t(chunk) * a.t.n_tokens * Hq + row;
         float *p = a.part_o + at * D + d0;
+        if constexpr (N == 1) {
+            __hip_atomic_store(p, o[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (d0 == 0) put_pair<true>(a.part_ml + 2 * at, m, l);
+        } else if (a.join_launch) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) p[i] = o[i];
-        if (d0 == 0) {
-            a.part_ml[2 * at] = m;
-            a.part_ml[2 * at + 1] = l;
+            for (int i = 0; i < N; i += 2) put_pair<false>(p + i, o[i], o[i + 1]);
+            if (d0 == 0) put_pair<false>(a.part_ml + 2 * at, m, l);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i += 2) put_pair<true>(p + i, o[i], o[i + 1]);
+            if (d0 == 0) put_pair<true>(a.part_ml + 2 * at, m, l);
         }
     }
 }
@@ -536,6 +567,81 @@ __device__ inline void plain_rows(const PageAttendArgs &a, const Item &it, int b
             }
         }
         put<T, D>(a, it, c, tok, h, lane * (D / 64), o, m, l);
+    }
+}
+
+// Joins the partials of an item's rows from first on, every `stride`th.  D / 4 threads hold a row, so several
+// rows, or several shares of one row's chunks, go side by side; shares meet in LDS in a fixed order.
+// lds: 256 float4 and 256 float2.
+template <class T, int D, bool kThrough>
+__device__ inline void join_rows(const PageAttendArgs &a, Item it, int g, int first, int rows, int lane, unsigned char *lds) {
+    constexpr int GT = D / 4, NG = 256 / GT;                 // threads a group, groups
+    const int t = threadIdx.x % GT, grp = threadIdx.x / GT, n = it.chunk1 - it.chunk0 + 1;
+    int side = 1;                                            // rows side by side: a power of two
+    while (side < rows && side < NG) side *= 2;
+    const int shares = NG / side, share = grp % shares;
+    float4 *so = reinterpret_cast<float4 *>(lds);
+    float2 *sm = reinterpret_cast<float2 *>(lds + 256 * sizeof(float4));
+    const int Hq = a.t.Hkv << a.group_shift;
+    const size_t step = size_t(a.t.n_tokens) * Hq;
+    for (int r0 = 0; r0 < rows; r0 += side) {
+        const int r = r0 + grp / shares, rw = first + (r < rows ? r : rows - 1);
+        const int tok = it.tok0 + (rw >> a.group_shift), h = (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1));
+        const size_t at = size_t(it.chunk0) * step + size_t(tok) * Hq + h;
+        float m = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int U = 4;
+        for (int c0 = share; c0 < n; c0 += U * shares) {     // chunks share, share + shares, ...
+            float2 ml[U], lo[U], hi[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * shares < n ? c0 + u * shares : n - 1;
+                ml[u] = get_pair<kThrough>(a.part_ml + 2 * (at + c * step));
+                lo[u] = get_pair<kThrough>(a.part_o + (at + c * step) * D + 4 * t);
+                hi[u] = get_pair<kThrough>(a.part_o + (at + c * step) * D + 4 * t + 2);
+            }
+            float mn = m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) mn = fmaxf(mn, ml[u].x);
+            const float mu = mn == -INFINITY ? 0.f : mn, f0 = exp2_fast(m - mu);
+            m = mn;
+            l *= f0;
+            o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (c0 + u * shares < n) {
+                    const float f = exp2_fast(ml[u].x - mu);
+                    l += f * ml[u].y;
+                    o.x += f * lo[u].x; o.y += f * lo[u].y; o.z += f * hi[u].x; o.w += f * hi[u].y;
+                }
+            }
+        }
+        if (shares > 1) {
+            so[threadIdx.x] = o;
+            if (t == 0) sm[grp] = make_float2(m, l);
+            __syncthreads();
+            if (share == 0) {
+                float mx = m;
+                for (int s = 1; s < shares; ++s) mx = fmaxf(mx, sm[grp + s].x);
+                const float mu = mx == -INFINITY ? 0.f : mx, f0 = exp2_fast(m - mu);
+                l *= f0;
+                o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+                for (int s = 1; s < shares; ++s) {
+                    const float f = exp2_fast(sm[grp + s].x - mu);
+                    const float4 x = so[threadIdx.x + s * GT];
+                    l += f * sm[grp + s].y;
+                    o.x += f * x.x; o.y += f * x.y; o.z += f * x.z; o.w += f * x.w;
+                }
+                m = mx;
+            }
+            __syncthreads();
+        }
+        if (share == 0 && r < rows) {
+            Item whole = it;
+            whole.chunk1 = whole.chunk0;                     // the output itself
+            const float x[4] = {o.x, o.y, o.z, o.w};
+            put<T, D>(a, whole, 0, tok, h, 4 * t, x, m, l);
+        }
     }
 }
 

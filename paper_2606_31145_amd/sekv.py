@@ -7,6 +7,7 @@ module loads the library and raises if it has not been built.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -735,6 +736,10 @@ class PageCache:
         self.k_scale, self.v_scale = k_scale, v_scale
         self.page_table, self.seq_len = page_table, seq_len
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_seen", None)              # to be checked again
+
     @classmethod
     def empty(cls, pd: PageDims, page_table, seq_len, device="cuda"):
         """Pools of zeros for pd."""
@@ -746,8 +751,15 @@ class PageCache:
         ks, vs = (torch.full(shape[:-1], 127, dtype=torch.uint8, device=device) for _ in "kv")
         return cls(k, v, page_table, seq_len, ks, vs)
 
+    def _tensors(self):
+        return self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table, self.seq_len
+
     def struct(self, pd: PageDims) -> PagesStruct:
-        """Checked against pd: types, sizes, one device."""
+        """The C view.  Types, sizes and devices are checked against pd when an attribute was set, a
+        tensor has moved or pd is another than in the last call."""
+        seen = (bytes(pd), *[None if x is None else x.data_ptr() for x in self._tensors()])
+        if seen == self._seen:
+            return self._struct
         rows = (pd.n_pages, pd.n_kv_heads, pd.page_size)
         want = _PAGE_STORAGE[pd.page_dtype] if pd.page_dtype in _PAGE_STORAGE else None
         dev = self.k_pages.device
@@ -760,28 +772,28 @@ class PageCache:
             if x is None and dt is torch.uint8:
                 continue
             _expect(x, name, dt, shape, dev)
-        return PagesStruct(_ptr(self.k_pages), _ptr(self.v_pages), _ptr(self.k_scale), _ptr(self.v_scale),
-                           _ptr(self.page_table), _ptr(self.seq_len))
+        object.__setattr__(self, "_struct", PagesStruct(*[_ptr(x) for x in self._tensors()]))
+        object.__setattr__(self, "_seen", seen)
+        return self._struct
 
 
 def _expect(x, name, dtype, shape, device):
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
-    if x.dtype != dtype or tuple(x.shape) != tuple(shape):
+    if x.dtype != dtype or x.shape != shape:
         raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, expected {dtype} {tuple(shape)}")
     if x.device != device:
         raise ValueError(f"{name} is on {x.device}, the pages on {device}")
 
 
-def _token_rows(pd: PageDims, x, name, heads, n_tokens, device):
-    """The token stride of [n_tokens][heads][d] rows that are contiguous within a token."""
-    _expect(x, name, _PAGE_STORAGE[pd.dtype], (n_tokens, heads, pd.head_dim), device)
-    d = pd.head_dim
-    if n_tokens == 0:
-        return heads * d
-    if x.stride(2) != 1 or (heads > 1 and x.stride(1) != d):
+def _token_rows(pd: PageDims, x, name, heads, device):
+    """(address, token stride) of [n_tokens][heads][d] rows that are contiguous within a token."""
+    d, n = pd.head_dim, x.shape[0]
+    _expect(x, name, _PAGE_STORAGE[pd.dtype], (n, heads, d), device)
+    s = x.stride()
+    if n and (s[2] != 1 or (heads > 1 and s[1] != d)):
         raise ValueError(f"{name}: a token's heads have to lie one after another")
-    return x.stride(0) if n_tokens > 1 else heads * d
+    return x.data_ptr(), s[0] if n > 1 else heads * d
 
 
 def _tok_start(pd: PageDims, tok_start, device):
@@ -789,12 +801,17 @@ def _tok_start(pd: PageDims, tok_start, device):
     return _ptr(tok_start)
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(device, stream):
-    """The device and stream context of a call: the caller's stream, else the device's current one."""
+    """The device and stream context of a call, and the stream's handle: the caller's stream, else the
+    device's current one."""
     if device.type != "cuda":
         raise ValueError("the pages have to be on a GPU")
     if stream is None:
-        return torch.cuda.device(device), torch.cuda.current_stream(device).cuda_stream
+        st = torch._C._cuda_getCurrentRawStream(device.index)
+        return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device), st
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     return torch.cuda.stream(stream), stream.cuda_stream
@@ -803,31 +820,30 @@ def _on(device, stream):
 def page_append(pd: PageDims, cache: PageCache, k, v, tok_start, ws: Workspace, stream=None):
     """sekv_page_append: stores k, v [n_tokens][Hkv][d] (tokens may be strided) in the pages."""
     cs, dev = cache.struct(pd), cache.k_pages.device
-    n = k.shape[0]
-    sk = _token_rows(pd, k, "k", pd.n_kv_heads, n, dev)
-    sv = _token_rows(pd, v, "v", pd.n_kv_heads, n, dev)
+    kp, sk = _token_rows(pd, k, "k", pd.n_kv_heads, dev)
+    vp, sv = _token_rows(pd, v, "v", pd.n_kv_heads, dev)
+    if len(k) != len(v):
+        raise ValueError(f"v: {len(v)} tokens, k has {len(k)}")
     ts = _tok_start(pd, tok_start, dev)
     ctx, st = _on(dev, stream)
     with ctx:
-        _check(LIB.sekv_page_append(ctypes.byref(pd), ctypes.byref(cs), k.data_ptr(), v.data_ptr(), sk, sv, ts, n,
-                                    ws.ptr, ws.nbytes, st))
+        _check(LIB.sekv_page_append(pd, cs, kp, vp, sk, sv, ts, len(k), ws.ptr, ws.nbytes, st))
 
 
 def page_read(pd: PageDims, cache: PageCache, max_tokens: int, ws: Workspace, keys=None, values=None, stream=None):
     """sekv_page_read: (keys, values) [B][Hkv][max_tokens][d]; rows behind a sequence's last token
     are left as given, zeros in tensors allocated here."""
-    cs, dev = cache.struct(pd), cache.k_pages.device
+    cs, dev, dt = cache.struct(pd), cache.k_pages.device, _PAGE_STORAGE[pd.dtype]
     shape = (pd.batch, pd.n_kv_heads, int(max_tokens), pd.head_dim)
     ctx, st = _on(dev, stream)
     with ctx:
         if keys is None:
-            keys = torch.zeros(shape, dtype=_PAGE_STORAGE[pd.dtype], device=dev)
+            keys = torch.zeros(shape, dtype=dt, device=dev)
         if values is None:
-            values = torch.zeros(shape, dtype=_PAGE_STORAGE[pd.dtype], device=dev)
-        _expect(keys, "keys", _PAGE_STORAGE[pd.dtype], shape, dev)
-        _expect(values, "values", _PAGE_STORAGE[pd.dtype], shape, dev)
-        _check(LIB.sekv_page_read(ctypes.byref(pd), ctypes.byref(cs), _ptr(keys), _ptr(values), int(max_tokens),
-                                  ws.ptr, ws.nbytes, st))
+            values = torch.zeros(shape, dtype=dt, device=dev)
+        _expect(keys, "keys", dt, shape, dev)
+        _expect(values, "values", dt, shape, dev)
+        _check(LIB.sekv_page_read(pd, cs, _ptr(keys), _ptr(values), int(max_tokens), ws.ptr, ws.nbytes, st))
     return keys, values
 
 
@@ -836,20 +852,19 @@ def page_attend(pd: PageDims, cache: PageCache, q, tok_start, ws: Workspace, out
     """sekv_page_attend: (out [n_tokens][Hq][d], lse float [n_tokens][Hq] or None) of the queries
     q [n_tokens][Hq][d] (tokens may be strided)."""
     cs, dev = cache.struct(pd), cache.k_pages.device
-    n = q.shape[0]
-    sq = _token_rows(pd, q, "q", pd.n_q_heads, n, dev)
+    qp, sq = _token_rows(pd, q, "q", pd.n_q_heads, dev)
     ts = _tok_start(pd, tok_start, dev)
     ctx, st = _on(dev, stream)
     with ctx:
         if out is None:
-            out = torch.empty((n, pd.n_q_heads, pd.head_dim), dtype=q.dtype, device=dev)
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        else:
+            _expect(out, "out", q.dtype, q.shape, dev)
         if lse is None and want_lse:
-            lse = torch.empty((n, pd.n_q_heads), dtype=torch.float32, device=dev)
-        _expect(out, "out", q.dtype, (n, pd.n_q_heads, pd.head_dim), dev)
-        if lse is not None:
-            _expect(lse, "lse", torch.float32, (n, pd.n_q_heads), dev)
-        _check(LIB.sekv_page_attend(ctypes.byref(pd), ctypes.byref(cs), q.data_ptr(), sq, ts, n, _ptr(out), _ptr(lse),
-                                    ws.ptr, ws.nbytes, st))
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
+        elif lse is not None:
+            _expect(lse, "lse", torch.float32, q.shape[:2], dev)
+        _check(LIB.sekv_page_attend(pd, cs, qp, sq, ts, len(q), _ptr(out), _ptr(lse), ws.ptr, ws.nbytes, st))
     return out, lse
 
 

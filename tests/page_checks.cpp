@@ -26,23 +26,26 @@ static void walk(const Tables &t, int Hkv, int gs, int64_t cap, int window, int 
     REQUIRE(l.splits >= 1 && l.splits <= 256 && l.target >= 1);
     REQUIRE((int64_t(t.n_tokens) << gs) * Hkv * l.splits <= partial_rows(t.n_tokens, Hkv, gs, cap, items));
     REQUIRE(partial_rows(t.n_tokens, Hkv, gs, cap, items) <= partial_rows(t.n_tokens + 1, Hkv, gs, cap, items));
+    if (l.splits > 1) REQUIRE(int64_t(t.n_tokens) * Hkv <= counter_words(Hkv, gs, items));
     std::vector<Seq> seq;
     uint64_t W = 0;
-    int mx = 0;
+    int mx = 0, T = 0;
     for (int b = 0; b < B; ++b) {
         seq.push_back(make_seq(t.start[b], t.start[b + 1], t.len[b], t.n_tokens, cap, window, gs));
         const Seq &s = seq.back();
         REQUIRE(s.start >= 0 && s.nq >= 0 && s.start + s.nq <= t.n_tokens);
         REQUIRE(s.lo >= 0 && s.lo % kChunkStep == 0 && s.len >= 0 && s.lo + int64_t(s.len) <= cap);
         W += uint64_t(s.tiles) * uint64_t(s.len);
+        T += s.tiles;
         mx = mx > s.len ? mx : s.len;
     }
-    const int chunk = l.splits == 1 ? 1 << 30 : chunk_length(W, mx, l.target, l.splits);
+    const int chunk = l.splits == 1 ? 1 << 30 : chunk_length(W, T, mx, Hkv, l.target, l.splits, join_in_launch(B, t.n_tokens, gs) ? kOverWide : kOverNarrow);
     REQUIRE(chunk % kChunkStep == 0);
     std::vector<std::vector<int>> seen(t.n_tokens);
     for (auto &v : seen) v.assign(size_t(cap), 0);
     std::vector<int> done(t.n_tokens, 0);
     int64_t pairs = 0;
+    bool wide = false;
     for (int b = 0; b < B; ++b) {
         const Seq &s = seq[b];
         const int n = chunks_of(s, chunk);
@@ -54,6 +57,7 @@ static void walk(const Tables &t, int Hkv, int gs, int64_t cap, int window, int 
                 if (it.idle) continue;
                 REQUIRE(it.rows >= 1 && it.rows <= (it.narrow ? kNarrowRows : kTileRows));
                 REQUIRE(it.tok0 >= 0 && it.n_tok >= 1 && it.tok0 + it.n_tok <= t.n_tokens && it.rows == it.n_tok << gs);
+                if (!it.narrow) wide = true;
                 REQUIRE(it.chunk0 >= 0 && it.chunk0 <= it.chunk1 && it.chunk1 < n);
                 REQUIRE(it.begin % 64 == 0 && it.begin >= 0 && it.end <= cap);
                 for (int i = 0; i < it.n_tok; ++i) {
@@ -66,6 +70,7 @@ static void walk(const Tables &t, int Hkv, int gs, int64_t cap, int window, int 
     }
     if (!good) return;
     REQUIRE(pairs <= l.pairs);
+    if (join_in_launch(B, t.n_tokens, gs) && t.n_tokens == t.start[B]) REQUIRE(wide);
     for (int b = 0; b < B; ++b)
         for (int i = t.start[b]; i < t.start[b + 1]; ++i) {
             REQUIRE(done[i] == 1);
