@@ -6,6 +6,8 @@
 // than one chunk leaves partials (m, l, o), which a second kernel joins.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "sekv_page_wide.h"
 
 #if !defined(SEKV_T) || !defined(SEKV_P) || !defined(SEKV_D)
@@ -112,32 +114,37 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
         }
         return valid;
     };
+    auto partial = [&](int pos, uint32_t valid) { return valid != 15u || pos < all_lo || pos + 63 > all_hi; };
     auto store = [&](int pos, uint32_t valid, int buf) {
-        if (valid != 15u || pos < all_lo || pos + 63 > all_hi)
-            bad |= st.mend(wave * 16, valid >> wave & 1 ? it.end - pos : 0, lane);
+        if (partial(pos, valid)) bad |= st.mend(wave * 16, valid >> wave & 1 ? it.end - pos : 0, lane);
         st.store(lds + buf * kTile, lds + (2 + buf) * kTile, wave * 16, lane);
     };
-    int mine = -1;
-    uint32_t valid = look(it.begin, &mine);
+    int mine = -1, pos = it.begin;
+    uint32_t valid = look(pos, &mine);
     st.load(a, mine, lane);
-    uint32_t ahead = look(it.begin + 64, &mine);
-    int buf = 0;
-    store(it.begin, valid, 0);
+    uint32_t ahead = look(pos + 64, &mine);
+    store(pos, valid, 0);
     __syncthreads();
-    for (int pos = it.begin; pos < it.end; pos += 64) {
+    const lds_bytes tile = (lds_bytes)lds;
+    // one tile from buffer kBuf, the next one into the other; false when that was the last
+    auto turn = [&](auto kBuf) {
+        constexpr int B = decltype(kBuf)::value;
         const bool more = pos + 64 < it.end;
         uint32_t after = 0;
         if (more) {
             st.load(a, mine, lane);
             after = look(pos + 128, &mine);
         }
-        r.step(a, lds + buf * kTile, lds + (2 + buf) * kTile, pos, valid, lane);
-        buf ^= 1;
-        if (more) store(pos + 64, ahead, buf);
+        if (wave * 32 < it.rows) r.step(a, tile + B * kTile, tile + (2 + B) * kTile, pos, valid, partial(pos, valid), lane);
+        if (more) store(pos + 64, ahead, 1 - B);
         __syncthreads();
+        pos += 64;
         valid = ahead;
         ahead = after;
-    }
+        return more;
+    };
+    if (it.begin < it.end)
+        while (turn(std::integral_constant<int, 0>{}) && turn(std::integral_constant<int, 1>{})) {}
     if (__syncthreads_or(bad)) return true;
     const int n = lane & 31, h = lane >> 5, rw = wave * 32 + n;
     const float l = r.l + across32(r.l);

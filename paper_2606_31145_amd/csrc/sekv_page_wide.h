@@ -21,12 +21,17 @@ namespace page {
 
 // Four rows of one column of a bf16 tile in LDS: within 16 lanes, lane i names 4 columns
 // 4 (i % 4) of row i / 4 and receives column i of the four rows.
-__device__ inline uint2 turn4(const unsigned char *p) {
+typedef __attribute__((address_space(3))) unsigned char *lds_bytes;      // so that constant offsets stay in the instruction
+__device__ inline uint2 turn4(lds_bytes p) {
     typedef short s4v __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s4v *lds_p;
-    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_p>(reinterpret_cast<uintptr_t>(p))));
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)p));
 }
-
+__device__ inline uint4 take16(lds_bytes p) {
+    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+    const u4v w = *(__attribute__((address_space(3))) const u4v *)p;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 template <int D> struct Swizzle {
     static constexpr int CH = D / 8;                   // 16-byte pieces a row
     static __device__ int key(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
@@ -151,14 +156,14 @@ struct Rows32 {
     }
 
     // V^T operand: 32 elements from 32 db on, the 16 keys of block kb
-    __device__ uint4 v_frag(const unsigned char *vt, int kb, int db) const {
+    __device__ uint4 v_frag(lds_bytes vt, int kb, int db) const {
         const uint2 x = turn4(vt + vaddr[0][db] + kb * (32 * D)), y = turn4(vt + vaddr[1][db] + kb * (32 * D));
         return make_uint4(x.x, x.y, y.x, y.y);
     }
 
-    // One tile: 64 keys from pos on; valid: which of its four blocks hold keys.
-    __device__ void step(const PageAttendArgs &a, const unsigned char *kt, const unsigned char *vt, int pos, uint32_t valid, int lane) {
-        if (pos > hi_any || pos + 63 < lo_any) return;
+    // One tile: 64 keys from pos on.  part: some column may not see some key, and `valid` says which of the
+    // four blocks hold keys.  The sum takes the weights before they are rounded: lse is a float.
+    __device__ void step(const PageAttendArgs &a, lds_bytes kt, lds_bytes vt, int pos, uint32_t valid, bool part, int lane) {
         const int h = lane >> 5;
         f16v s[2];
 #pragma unroll
@@ -166,10 +171,8 @@ struct Rows32 {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[j][r] = 0.f;
 #pragma unroll
-            for (int c = 0; c < QS; ++c)
-                s[j] = mma32(*reinterpret_cast<const uint4 *>(kt + kaddr[c] + j * (64 * D)), q[c], s[j]);
+            for (int c = 0; c < QS; ++c) s[j] = mma32(take16(kt + kaddr[c] + j * (64 * D)), q[c], s[j]);
         }
-        const bool part = valid != 15u || pos < lo_all || pos + 63 > hi_all;
         if (part) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -195,20 +198,22 @@ struct Rows32 {
         }
         const float mu = m == -INFINITY ? 0.f : m;
         uint4 pf[4];
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float sum = 0.f;
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[j][r] = exp2_fast(fmaf(s[j][r], a.scale_log2, -mu));
-                sum += s[j][r];
+            for (int u = 0; u < 2; ++u) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 8 * u + 2 * i;
+                    const float x = exp2_fast(fmaf(s[j][r], a.scale_log2, -mu)), y = exp2_fast(fmaf(s[j][r + 1], a.scale_log2, -mu));
+                    sum[i & 1] += x + y;
+                    w[i] = bf16_pack(x, y);
+                }
+                pf[2 * j + u] = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            l += sum;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                pf[2 * j + u] = make_uint4(bf16_pack(s[j][8 * u], s[j][8 * u + 1]), bf16_pack(s[j][8 * u + 2], s[j][8 * u + 3]),
-                                           bf16_pack(s[j][8 * u + 4], s[j][8 * u + 5]), bf16_pack(s[j][8 * u + 6], s[j][8 * u + 7]));
-        }
+        l += sum[0] + sum[1];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
