@@ -103,26 +103,29 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     const int64_t all_lo = w, all_hi = it.p0;                // keys that every row of the item sees
     Stage<P, D> st;
     bool bad = false;
-    // the four blocks of a tile: mine to fetch, all of them to know which hold keys
-    auto look = [&](int pos, int *mine) {
-        uint32_t valid = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = key_block(a, b, g, pos + 16 * j, it.end, lane);
-            valid |= row >= 0 ? 1u << j : 0u;
-            if (j == wave) *mine = row;
-        }
-        return valid;
+    // the four blocks of a tile, one a lane: their page, read two tiles ahead, then mine to fetch and which of
+    // them hold keys
+    auto page_of = [&](int pos) {
+        const int p = pos + 16 * (lane & 3);
+        return p < it.end ? a.t.table[int64_t(b) * a.t.max_pages + (p >> a.t.page_shift)] : -1;
+    };
+    auto rows_of = [&](int pos, int page, int *mine) {
+        const int p = pos + 16 * (lane & 3), row = block_row(page, a.t.n_pages, a.t.Hkv, g, a.t.page_shift, p);
+        if (row < 0 && p < it.end && lane < 4) flag(a.t);
+        *mine = __builtin_amdgcn_readlane(row, wave);
+        return uint32_t(__ballot(row >= 0)) & 15u;
     };
     auto partial = [&](int pos, uint32_t valid) { return valid != 15u || pos < all_lo || pos + 63 > all_hi; };
     auto store = [&](int pos, uint32_t valid, int buf) {
         if (partial(pos, valid)) bad |= st.mend(wave * 16, valid >> wave & 1 ? it.end - pos : 0, lane);
         st.store(lds + buf * kTile, lds + (2 + buf) * kTile, wave * 16, lane);
     };
-    int mine = -1, pos = it.begin;
-    uint32_t valid = look(pos, &mine);
+    int pos = it.begin;
+    int mine = -1;
+    uint32_t valid = rows_of(pos, page_of(pos), &mine);
     st.load(a, mine, lane);
-    uint32_t ahead = look(pos + 64, &mine);
+    int page = page_of(pos + 64);
+    uint32_t ahead = 0;
     store(pos, valid, 0);
     __syncthreads();
     const lds_bytes tile = (lds_bytes)lds;
@@ -130,19 +133,21 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     auto turn = [&](auto kBuf) {
         constexpr int B = decltype(kBuf)::value;
         const bool more = pos + 64 < it.end;
-        uint32_t after = 0;
         if (more) {
+            ahead = rows_of(pos + 64, page, &mine);
             st.load(a, mine, lane);
-            after = look(pos + 128, &mine);
+            page = page_of(pos + 128);
         }
         if (wave * 32 < it.rows) r.step(a, tile + B * kTile, tile + (2 + B) * kTile, pos, valid, partial(pos, valid), lane);
         if (more) store(pos + 64, ahead, 1 - B);
         __syncthreads();
         pos += 64;
         valid = ahead;
-        ahead = after;
         return more;
     };
+    // Two waves share a SIMD, and in step they would want the matrix unit and then the vector unit at the same
+    // time: one goes first, by its slot, and the other fills what it leaves.
+    if (__builtin_amdgcn_s_getreg(6148) & 1) __builtin_amdgcn_s_setprio(1);
     if (it.begin < it.end)
         while (turn(std::integral_constant<int, 0>{}) && turn(std::integral_constant<int, 1>{})) {}
     if (__syncthreads_or(bad)) return true;
