@@ -170,7 +170,7 @@ sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages
     a.window = dims->window > 0 ? dims->window : 0x7fffffff;
     a.scale_log2 = float(dims->softmax_scale * 1.4426950408889634074);
     const sekv::page::Launch l = plan(dims, n_tokens);
-    a.splits = l.splits; a.target = l.target; a.pairs = l.pairs;
+    a.splits = l.splits; a.target = l.target; a.tiles = l.tiles; a.pairs = l.pairs;
     a.join_launch = sekv::page::join_in_launch(dims->batch, n_tokens, a.group_shift);
     a.arrived = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(ws) + sizeof(sekv::WsHeader));
     a.part_o = reinterpret_cast<float *>(a.arrived + counters(dims));

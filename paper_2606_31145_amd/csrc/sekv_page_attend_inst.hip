@@ -21,41 +21,44 @@ using namespace page;
 
 constexpr int kThreads = 256, kWaves = 4;
 
-// At most 16 rows: every wave takes all of them, and every fourth step of the keys.  True when the item
-// has to be done again by plain_rows.
-template <class T, class P, int D>
+// At most 16 NB rows: every wave takes all of them, and every fourth step of the keys.  True when the
+// item has to be done again by plain_rows.
+template <class T, class P, int D, int NB>
 __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
-    using R = Rows16<T, P, D, 1>;
-    constexpr int VE = R::VE, RS = D + 4, kKeys = R::Tile::kKeys;
+    using R = Rows16<T, P, D, NB>;
+    constexpr int VE = R::VE, RS = D + 4, kKeys = R::Tile::kKeys, N = 16 * NB;
     R r;
     r.init(a, it, g, 0, lane);
     bool bad = false;
     r.run(a, it, b, g, it.begin + wave * kKeys, kKeys * kWaves, &bad, lane);
     // the four waves' parts, joined through LDS
-    float *ml = reinterpret_cast<float *>(lds), *so = ml + kWaves * 32;
+    float *ml = reinterpret_cast<float *>(lds), *so = ml + kWaves * 2 * N;
     const int n = lane & 15, gq = lane >> 4;
-    const float l = r.sum(0);
-    if (gq == 0) {
-        ml[wave * 32 + n] = r.m[0];
-        ml[wave * 32 + 16 + n] = l;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const float l = r.sum(nb);
+        if (gq == 0) {
+            ml[wave * 2 * N + 16 * nb + n] = r.m[nb];
+            ml[wave * 2 * N + N + 16 * nb + n] = l;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) so[(wave * N + 16 * nb + n) * RS + VE * (4 * gq + i) + e] = r.o[nb][e][i];
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) so[(wave * 16 + n) * RS + VE * (4 * gq + i) + e] = r.o[0][e][i];
     if (__syncthreads_or(bad)) return true;
-    const int rw = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VE;
-    if (rw < it.rows) {
+    const int d0 = (threadIdx.x & 15) * VE;
+    for (int rw = threadIdx.x >> 4; rw < it.rows; rw += 16) {
         float m = -INFINITY, sum = 0.f, o[VE] = {};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w * 32 + rw]);
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w * 2 * N + rw]);
         const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float f = exp2_fast(ml[w * 32 + rw] - mu);
-            sum += f * ml[w * 32 + 16 + rw];
+            const float f = exp2_fast(ml[w * 2 * N + rw] - mu);
+            sum += f * ml[w * 2 * N + N + rw];
 #pragma unroll
-            for (int e = 0; e < VE; ++e) o[e] += f * so[(w * 16 + rw) * RS + d0 + e];
+            for (int e = 0; e < VE; ++e) o[e] += f * so[(w * N + rw) * RS + d0 + e];
         }
         put<T, D>(a, it, c, it.tok0 + (rw >> a.group_shift), (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1)), d0, o, m, sum);
     }
@@ -168,7 +171,7 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
 
 template <class T, class P, int D>
 __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
-    constexpr int kNarrowLds = (kWaves * 32 + kWaves * 16 * (D + 4)) * 4, kWideLds = T::kBytes == 2 ? 4 * 64 * D * 2 : 0;
+    constexpr int kNarrowLds = kWaves * kNarrowRows * (2 + D + 4) * 4, kWideLds = T::kBytes == 2 ? 4 * 64 * D * 2 : 0;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kNarrowLds > kWideLds ? kNarrowLds : kWideLds];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (blockIdx.x == 0)                                     // tables that cannot be
@@ -184,7 +187,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
     Item it;
     if (!chunk || !find_item(a, blockIdx.x / a.t.Hkv, lane, chunk, &b, &c, &it)) return;
     bool again;
-    if (it.narrow) again = narrow<T, P, D>(a, it, b, g, c, lane, wave, lds);
+    if (it.narrow && it.rows <= 16) again = narrow<T, P, D, 1>(a, it, b, g, c, lane, wave, lds);
+    else if (it.narrow) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);
     else if constexpr (T::kBytes == 2) again = wide_bf16<P, D>(a, it, b, g, c, lane, wave, lds);
     else again = wide_f32<P, D>(a, it, b, g, c, lane, wave);
     if (again) plain_rows<T, P, D>(a, it, b, g, c, lane, wave);
@@ -203,25 +207,25 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
     join_rows<T, D, true>(a, it, g, 0, it.rows, lane, lds);
 }
 
-// Joins the partials of a token's query heads of one KV head.
+// Joins the partials of 16 rows of a tile at a time.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
+    constexpr int kRows = 16, kParts = kTileRows / kRows;
     __shared__ __attribute__((aligned(16))) unsigned char lds[256 * (sizeof(float4) + sizeof(float2))];
-    const int lane = threadIdx.x & 63, tok = blockIdx.x / a.t.Hkv, g = blockIdx.x % a.t.Hkv;
-    const int chunk = find_chunk(a, lane);
-    if (!chunk) return;
-    int lo = 0, hi = a.t.B;                                  // the last b with tok_start[b] <= tok
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.t.tok_start[mid] <= tok) lo = mid; else hi = mid;
+    const int lane = threadIdx.x & 63;
+    int tiles = 0, longest = 0;
+    const int chunk = find_chunk(a, lane, &tiles, &longest);
+    if (!chunk || longest <= chunk) return;                  // nothing was cut
+    const int64_t all = int64_t(tiles) * a.t.Hkv * kParts;
+    for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
+        const int g = int(u % a.t.Hkv), part = int(u / a.t.Hkv % kParts);
+        int b = 0, c = 0;
+        Item it;
+        find_item<true>(a, uint32_t(u / a.t.Hkv / kParts), lane, chunk, &b, &c, &it);
+        const int left = it.rows - part * kRows;
+        if (it.chunk0 == it.chunk1 || left <= 0) continue;
+        join_rows<T, D, false>(a, it, g, part * kRows, left < kRows ? left : kRows, lane, lds);
     }
-    const Seq s = load_seq(a, lo);
-    if (tok < s.start || tok >= s.start + s.nq) return;
-    const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
-    const int tile = (s.nq << a.group_shift) <= kNarrowRows ? 0 : ((tok - s.start) << a.group_shift) / kTileRows;
-    const Item it = make_item(s, tile, 0, chunk, cap, a.window, a.group_shift);
-    if (it.chunk0 == it.chunk1) return;
-    join_rows<T, D, false>(a, it, g, (tok - it.tok0) << a.group_shift, 1 << a.group_shift, lane, lds);
 }
 
 }  // namespace
@@ -235,7 +239,8 @@ hipError_t SEKV_NAME(SEKV_T, SEKV_P, SEKV_D)(const PageAttendArgs &a, hipStream_
     hipLaunchKernelGGL((attend_kernel<T, P, SEKV_D>), dim3(unsigned(a.pairs * a.t.Hkv)), dim3(kThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1 || !a.join_launch) return e;
-    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned(a.t.n_tokens) * unsigned(a.t.Hkv)), dim3(kThreads), 0, s, a);
+    const int64_t parts = a.tiles * a.t.Hkv * (page::kTileRows / 16);
+    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned(parts < 1024 ? parts : 1024)), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -2,7 +2,7 @@
 // arithmetic only, also compiled for the host, where a test walks through it.
 //
 // Work items.  The query rows of a sequence and KV head (its new tokens x its query heads) are cut
-// into tiles of kTileRows, or are one narrow tile when there are at most kNarrowRows.  A tile's keys
+// into tiles: of kTileRows, or, when there are at most kFewRows, into narrow tiles of kNarrowRows.  A tile's keys
 // are cut into chunks so that few rows over many keys still fill the device.  The chunk length is
 // found from the device's tables, the same for the whole call: with T_b tiles and L_b keys of
 // sequence b, W = sum T_b L_b, chunk >= max(W / target, max L_b / splits) in steps of kChunkStep
@@ -29,7 +29,8 @@
 namespace sekv {
 namespace page {
 
-constexpr int kNarrowRows = 16;    // columns of a 16-wide matrix tile
+constexpr int kNarrowRows = 32;    // one or two 16-wide matrix tiles
+constexpr int kFewRows = 64;       // rows of two narrow tiles, which read the keys twice, the second time from cache
 constexpr int kTileRows = 128;     // 32 rows for each of four waves
 constexpr int kChunkStep = 128;    // keys: a step of 32 for each of four waves
 constexpr int kSlots = 512;        // workgroups that run at once: two on each of 256 compute units
@@ -64,7 +65,8 @@ SEKV_HD Seq make_seq(int start, int end, int seq_len, int n_tokens, int64_t cap,
     s.lo = int(lo < hi ? lo : 0);
     s.len = s.nq && lo < hi ? int(hi - lo) : 0;
     const int rows = s.nq << group_shift;
-    s.tiles = rows <= kNarrowRows ? (rows > 0) : (rows + kTileRows - 1) / kTileRows;
+    const int per = rows <= kFewRows ? kNarrowRows : kTileRows;
+    s.tiles = (rows + per - 1) / per;
     return s;
 }
 
@@ -108,8 +110,8 @@ struct Item {
 
 SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, int window, int group_shift) {
     Item it;
-    it.narrow = (s.nq << group_shift) <= kNarrowRows;
-    const int per = it.narrow ? s.nq : kTileRows >> group_shift;
+    it.narrow = (s.nq << group_shift) <= kFewRows;
+    const int per = (it.narrow ? kNarrowRows : kTileRows) >> group_shift;
     const int t0 = tile * per, left = s.nq - t0;
     it.tok0 = s.start + t0;
     it.n_tok = left < per ? left : per;
@@ -137,8 +139,17 @@ SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, in
 struct Launch {
     int splits;           // chunks a tile may have
     int target;           // (tile, chunk) pairs aimed at
+    int64_t tiles;        // tiles of a KV head at most
     int64_t pairs;        // (tile, chunk) pairs at most
 };
+
+// One tile a sequence that has tokens, another one for those of more than kNarrowRows and at most kFewRows
+// rows, and one for every kTileRows rows.
+SEKV_HD int64_t most_tiles(int batch, int n_tokens, int group_shift) {
+    const int64_t rows = int64_t(n_tokens) << group_shift, n = batch < n_tokens ? batch : n_tokens;
+    const int64_t second = rows / (kNarrowRows + 1);
+    return n + (second < n ? second : n) + rows / kTileRows;
+}
 
 SEKV_HD int most_splits(int64_t cap) {
     const int64_t n = (cap + kChunkStep - 1) / kChunkStep;
@@ -152,8 +163,8 @@ SEKV_HD Launch plan_launch(int batch, int n_tokens, int Hkv, int group_shift, in
     const int64_t s = (int64_t(l.target) * kTileRows + r - 1) / r;
     const int most = most_splits(cap);
     l.splits = int(s < most ? s : most);
-    const int64_t tiles = (batch < n_tokens ? batch : n_tokens) + rows / kTileRows;
-    l.pairs = tiles + (l.splits > 1 ? l.target : 0);
+    l.tiles = most_tiles(batch, n_tokens, group_shift);
+    l.pairs = l.tiles + (l.splits > 1 ? l.target : 0);
     return l;
 }
 // Rows of partials (of all heads) that any call of up to n_tokens tokens needs: splits * rows is at
@@ -171,10 +182,10 @@ SEKV_HD int64_t counter_words(int Hkv, int group_shift, int items) {
     return (int64_t((items + Hkv - 1) / Hkv) * kTileRows >> group_shift) * Hkv;
 }
 // Whether the partials go to a second kernel.  Joining in the last workgroup of a tile saves a launch but
-// leaves a tile of 128 rows to one compute unit, so it is for tiles that are probably narrow; more new
-// tokens than narrow tiles hold mean that some tile is not.
+// leaves a tile of 128 rows to one compute unit, so it is for tiles that are probably narrow; more rows
+// than sequences of narrow tiles hold mean that some tile is not.
 SEKV_HD bool join_in_launch(int batch, int n_tokens, int group_shift) {
-    return (int64_t(n_tokens) << group_shift) > int64_t(batch) * kNarrowRows;
+    return (int64_t(n_tokens) << group_shift) > int64_t(batch) * kFewRows;
 }
 
 }  // namespace page

@@ -54,7 +54,7 @@ struct PageAttendArgs {
     int32_t group_shift;       // log2(Hq / Hkv)
     int32_t window;            // > 0; 2^31 - 1: none
     int32_t splits, target;    // see sekv_page_index.h
-    int64_t pairs;
+    int64_t tiles, pairs;
     float scale_log2;          // softmax_scale * log2(e)
     int32_t join_launch;       // partials are joined by a second kernel, not by a tile's last workgroup
     uint32_t *arrived;         // [n_tokens][Hkv] by a tile's first token: its chunks that are done; zero between calls

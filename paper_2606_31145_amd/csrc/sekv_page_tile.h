@@ -55,7 +55,7 @@ __device__ inline Seq load_seq(const PageAttendArgs &a, int b) {
 
 // The call's chunk length: three sums over the batch.  0 where tok_start does not ascend within the new
 // tokens: rows could then belong to two sequences, and a tile's counter to two tiles.
-__device__ inline int find_chunk(const PageAttendArgs &a, int lane) {
+__device__ inline int find_chunk(const PageAttendArgs &a, int lane, int *tiles = nullptr, int *longest = nullptr) {
     if (a.splits == 1) return 1 << 30;
     uint64_t W = 0;
     int mx = 0, T = 0;
@@ -78,12 +78,16 @@ __device__ inline int find_chunk(const PageAttendArgs &a, int lane) {
         }
     }
     W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
-    return chunk_length(W, __builtin_amdgcn_readfirstlane(T), __builtin_amdgcn_readfirstlane(mx), a.t.Hkv, a.target,
-                        a.splits, a.join_launch ? kOverWide : kOverNarrow);
+    T = __builtin_amdgcn_readfirstlane(T);
+    mx = __builtin_amdgcn_readfirstlane(mx);
+    if (tiles) *tiles = T;
+    if (longest) *longest = mx;
+    return chunk_length(W, T, mx, a.t.Hkv, a.target, a.splits, a.join_launch ? kOverWide : kOverNarrow);
 }
 
 // Pair x of the call: sequences in order, chunks of a sequence in order, tiles last first (the later
-// tokens of a chunk see more keys).
+// tokens of a chunk see more keys).  kTiles: tile x instead, as its first chunk's item.
+template <bool kTiles = false>
 __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, int chunk, int *b_out, int *c_out, Item *it) {
     const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
     uint32_t before = 0;
@@ -91,7 +95,7 @@ __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, 
         uint32_t n = 0;
         if (b0 + lane < a.t.B) {
             const Seq s = load_seq(a, b0 + lane);
-            n = uint32_t(s.tiles) * uint32_t(chunks_of(s, chunk));
+            n = uint32_t(s.tiles) * uint32_t(kTiles ? 1 : chunks_of(s, chunk));
         }
         uint32_t incl = n;
         if (a.t.B > 1) {

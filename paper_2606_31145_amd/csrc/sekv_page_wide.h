@@ -173,6 +173,14 @@ struct Rows32 {
 #pragma unroll
             for (int c = 0; c < QS; ++c) s[j] = mma32(take16(kt + kaddr[c] + j * (64 * D)), q[c], s[j]);
         }
+        // a piece of keys asked for four products ahead
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * QS - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         if (part) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -218,6 +226,14 @@ struct Rows32 {
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
             for (int db = 0; db < DB; ++db) o[db] = mma32(v_frag(vt, kb, db), pf[kb], o[db]);
+        // and the values two products ahead
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * DB - 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
     }
 };
 

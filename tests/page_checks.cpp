@@ -69,7 +69,7 @@ static void walk(const Tables &t, int Hkv, int gs, int64_t cap, int window, int 
             }
     }
     if (!good) return;
-    REQUIRE(pairs <= l.pairs);
+    REQUIRE(pairs <= l.pairs && T <= l.tiles);
     if (join_in_launch(B, t.n_tokens, gs) && t.n_tokens == t.start[B]) REQUIRE(wide);
     for (int b = 0; b < B; ++b)
         for (int i = t.start[b]; i < t.start[b + 1]; ++i) {
