@@ -175,7 +175,7 @@ sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages
     a.arrived = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(ws) + sizeof(sekv::WsHeader));
     a.part_o = reinterpret_cast<float *>(a.arrived + counters(dims));
     a.part_ml = a.part_o + size_t(l.splits) * n_tokens * dims->n_q_heads * dims->head_dim;
-    if (l.pairs * dims->n_kv_heads > (int64_t(1) << 23))
+    if (sekv::page::blocks_of(l.pairs, dims->n_kv_heads) > (int64_t(1) << 23))
         return fail(SEKV_ERR_UNSUPPORTED, "%d new tokens of %d heads in one call", n_tokens, dims->n_q_heads);
     hipError_t e = l.splits > 1 ? sekv::ws_prepare_pages(ws, ws_bytes, counters(dims), stream) : hipSuccess;
     if (e != hipSuccess) return fail(SEKV_ERR_HIP, "workspace zero kernel: %s", hipGetErrorString(e));

@@ -182,10 +182,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
                 (s.nq && a.t.seq_len[b] > cap))
                 flag(a.t);
         }
-    const int g = blockIdx.x % a.t.Hkv, chunk = find_chunk(a, lane);
-    int b = 0, c = 0;
+    const Plan plan = make_plan(a, lane);
+    int b = 0, c = 0, g = 0;
+    const uint32_t x = place_of(blockIdx.x, a.t.Hkv, &g);
     Item it;
-    if (!chunk || !find_item(a, blockIdx.x / a.t.Hkv, lane, chunk, &b, &c, &it)) return;
+    if (!plan.chunk || !find_item(a, x, lane, plan, &b, &c, &it)) return;
     bool again;
     if (it.narrow && it.rows <= 16) again = narrow<T, P, D, 1>(a, it, b, g, c, lane, wave, lds);
     else if (it.narrow) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);
@@ -213,15 +214,14 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
     constexpr int kRows = 16, kParts = kTileRows / kRows;
     __shared__ __attribute__((aligned(16))) unsigned char lds[256 * (sizeof(float4) + sizeof(float2))];
     const int lane = threadIdx.x & 63;
-    int tiles = 0, longest = 0;
-    const int chunk = find_chunk(a, lane, &tiles, &longest);
-    if (!chunk || longest <= chunk) return;                  // nothing was cut
-    const int64_t all = int64_t(tiles) * a.t.Hkv * kParts;
+    const Plan plan = make_plan(a, lane);
+    if (!plan.chunk || plan.longest <= plan.chunk) return;   // nothing was cut
+    const int64_t all = int64_t(plan.tiles) * a.t.Hkv * kParts;
     for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
         const int g = int(u % a.t.Hkv), part = int(u / a.t.Hkv % kParts);
         int b = 0, c = 0;
         Item it;
-        find_item<true>(a, uint32_t(u / a.t.Hkv / kParts), lane, chunk, &b, &c, &it);
+        find_item<true>(a, uint32_t(u / a.t.Hkv / kParts), lane, plan, &b, &c, &it);
         const int left = it.rows - part * kRows;
         if (it.chunk0 == it.chunk1 || left <= 0) continue;
         join_rows<T, D, false>(a, it, g, part * kRows, left < kRows ? left : kRows, lane, lds);
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
 hipError_t SEKV_NAME(SEKV_T, SEKV_P, SEKV_D)(const PageAttendArgs &a, hipStream_t s) {
     using T = page::SEKV_T;
     using P = page::SEKV_P;
-    hipLaunchKernelGGL((attend_kernel<T, P, SEKV_D>), dim3(unsigned(a.pairs * a.t.Hkv)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((attend_kernel<T, P, SEKV_D>), dim3(unsigned(page::blocks_of(a.pairs, a.t.Hkv))), dim3(kThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1 || !a.join_launch) return e;
     const int64_t parts = a.tiles * a.t.Hkv * (page::kTileRows / 16);

@@ -188,5 +188,21 @@ SEKV_HD bool join_in_launch(int batch, int n_tokens, int group_shift) {
     return (int64_t(n_tokens) << group_shift) > int64_t(batch) * kFewRows;
 }
 
+// Workgroup -> (pair, KV head).  Consecutive workgroups go to the chip's 8 dies in turn, each with a cache of
+// its own, and neighbouring pairs read the same keys.  With 8 heads a head stays on a die by itself; with 1, 2
+// or 4 a die takes kNear neighbouring pairs of a head.
+constexpr int kDies = 8, kNear = 8;
+SEKV_HD bool few_heads(int Hkv) { return Hkv == 1 || Hkv == 2 || Hkv == 4; }
+SEKV_HD int64_t blocks_of(int64_t pairs, int Hkv) {
+    const int64_t group = few_heads(Hkv) ? kDies / Hkv * kNear : 1;
+    return (pairs + group - 1) / group * group * Hkv;
+}
+SEKV_HD uint32_t place_of(uint32_t block, int Hkv, int *g) {
+    *g = int(block % uint32_t(Hkv));
+    if (!few_heads(Hkv)) return block / uint32_t(Hkv);
+    const uint32_t side = kDies / Hkv, die = block % kDies, turn = block / kDies;
+    return turn / kNear * (side * kNear) + die / uint32_t(Hkv) * kNear + turn % kNear;
+}
+
 }  // namespace page
 }  // namespace sekv

@@ -53,21 +53,46 @@ __device__ inline Seq load_seq(const PageAttendArgs &a, int b) {
                     a.window, a.group_shift);
 }
 
-// The call's chunk length: three sums over the batch.  0 where tok_start does not ascend within the new
-// tokens: rows could then belong to two sequences, and a tile's counter to two tiles.
-__device__ inline int find_chunk(const PageAttendArgs &a, int lane, int *tiles = nullptr, int *longest = nullptr) {
-    if (a.splits == 1) return 1 << 30;
+// One lane's sequence in all lanes.
+__device__ inline Seq of_lane(const Seq &s, int l) {
+    Seq r;
+    r.start = __builtin_amdgcn_readlane(s.start, l);
+    r.nq = __builtin_amdgcn_readlane(s.nq, l);
+    r.first = int64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(s.first), l)) |
+                      uint64_t(uint32_t(__builtin_amdgcn_readlane(uint32_t(uint64_t(s.first) >> 32), l))) << 32);
+    r.lo = __builtin_amdgcn_readlane(s.lo, l);
+    r.len = __builtin_amdgcn_readlane(s.len, l);
+    r.tiles = __builtin_amdgcn_readlane(s.tiles, l);
+    return r;
+}
+
+// What every wave finds out about the call for itself.
+struct Plan {
+    Seq mine;             // sequence `lane`: the tables of up to 64 sequences are read once
+    int chunk;            // 0 where tok_start does not ascend within the new tokens: rows could then belong to
+                          // two sequences, and a tile's counter to two tiles
+    int tiles, longest;   // of a KV head; keys of the longest sequence (where chunks may be cut)
+};
+
+__device__ inline Plan make_plan(const PageAttendArgs &a, int lane) {
+    Plan p;
     uint64_t W = 0;
     int mx = 0, T = 0;
     bool wrong = false;
     for (int b = lane; b < a.t.B; b += 64) {
-        const Seq s = load_seq(a, b);
-        wrong |= a.t.tok_start[b] != s.start || a.t.tok_start[b + 1] != s.start + s.nq;
+        const int from = a.t.tok_start[b], to = a.t.tok_start[b + 1];
+        const Seq s = make_seq(from, to, a.t.seq_len[b], a.t.n_tokens, int64_t(a.t.max_pages) << a.t.page_shift, a.window,
+                               a.group_shift);
+        if (b < 64) p.mine = s;
+        wrong |= from != s.start || to != s.start + s.nq;
         W += uint64_t(s.tiles) * uint64_t(s.len);
         T += s.tiles;
         mx = mx > s.len ? mx : s.len;
     }
-    if (__any(wrong)) return 0;
+    p.chunk = 1 << 30;
+    if (a.splits == 1) return p;
+    p.chunk = 0;
+    if (__any(wrong)) return p;
     if (a.t.B > 1) {
 #pragma unroll
         for (int k = 1; k < 64; k *= 2) {
@@ -78,24 +103,24 @@ __device__ inline int find_chunk(const PageAttendArgs &a, int lane, int *tiles =
         }
     }
     W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
-    T = __builtin_amdgcn_readfirstlane(T);
-    mx = __builtin_amdgcn_readfirstlane(mx);
-    if (tiles) *tiles = T;
-    if (longest) *longest = mx;
-    return chunk_length(W, T, mx, a.t.Hkv, a.target, a.splits, a.join_launch ? kOverWide : kOverNarrow);
+    p.tiles = __builtin_amdgcn_readfirstlane(T);
+    p.longest = __builtin_amdgcn_readfirstlane(mx);
+    p.chunk = chunk_length(W, p.tiles, p.longest, a.t.Hkv, a.target, a.splits, a.join_launch ? kOverWide : kOverNarrow);
+    return p;
 }
 
 // Pair x of the call: sequences in order, chunks of a sequence in order, tiles last first (the later
 // tokens of a chunk see more keys).  kTiles: tile x instead, as its first chunk's item.
 template <bool kTiles = false>
-__device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, int chunk, int *b_out, int *c_out, Item *it) {
+__device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, const Plan &p, int *b_out, int *c_out, Item *it) {
     const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
     uint32_t before = 0;
     for (int b0 = 0; b0 < a.t.B; b0 += 64) {
         uint32_t n = 0;
+        Seq s = p.mine;
         if (b0 + lane < a.t.B) {
-            const Seq s = load_seq(a, b0 + lane);
-            n = uint32_t(s.tiles) * uint32_t(kTiles ? 1 : chunks_of(s, chunk));
+            if (b0 > 0) s = load_seq(a, b0 + lane);
+            n = uint32_t(s.tiles) * uint32_t(kTiles ? 1 : chunks_of(s, p.chunk));
         }
         uint32_t incl = n;
         if (a.t.B > 1) {
@@ -109,11 +134,10 @@ __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, 
         if (past) {
             const int l = __ffsll(past) - 1;
             const uint32_t in = x - before - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l));
-            const int b = b0 + l;
-            const Seq s = load_seq(a, b);
-            *b_out = b;
+            s = of_lane(s, l);
+            *b_out = b0 + l;
             *c_out = int(in / uint32_t(s.tiles));
-            *it = make_item(s, s.tiles - 1 - int(in % uint32_t(s.tiles)), *c_out, chunk, cap, a.window, a.group_shift);
+            *it = make_item(s, s.tiles - 1 - int(in % uint32_t(s.tiles)), *c_out, p.chunk, cap, a.window, a.group_shift);
             return !it->idle;
         }
         before += __builtin_amdgcn_readlane(incl, 63);

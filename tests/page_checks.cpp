@@ -27,6 +27,17 @@ static void walk(const Tables &t, int Hkv, int gs, int64_t cap, int window, int 
     REQUIRE((int64_t(t.n_tokens) << gs) * Hkv * l.splits <= partial_rows(t.n_tokens, Hkv, gs, cap, items));
     REQUIRE(partial_rows(t.n_tokens, Hkv, gs, cap, items) <= partial_rows(t.n_tokens + 1, Hkv, gs, cap, items));
     if (l.splits > 1) REQUIRE(int64_t(t.n_tokens) * Hkv <= counter_words(Hkv, gs, items));
+    if (good) {                                          // every (pair, head) is some workgroup's, once
+        const int64_t n = blocks_of(l.pairs, Hkv);
+        std::vector<int> got(size_t(n) , 0);
+        for (int64_t i = 0; i < n; ++i) {
+            int g = -1;
+            const int64_t x = place_of(uint32_t(i), Hkv, &g);
+            REQUIRE(g >= 0 && g < Hkv && x >= 0 && x * Hkv + g < n);
+            got[size_t(x * Hkv + g)] += 1;
+        }
+        for (int v : got) REQUIRE(v == 1);
+    }
     std::vector<Seq> seq;
     uint64_t W = 0;
     int mx = 0, T = 0;
@@ -83,7 +94,7 @@ int main() {
     std::mt19937 r(7);
     auto in = [&](int a, int b) { return int(r() % unsigned(b - a + 1)) + a; };
     for (int trial = 0; trial < 3000; ++trial) {
-        const int B = in(1, 7), gs = in(0, 3), Hkv = in(1, 5), shift = in(4, 7), max_pages = in(1, 1 + (3000 >> shift));
+        const int B = in(1, 7), gs = in(0, 3), Hkv = in(1, 9), shift = in(4, 7), max_pages = in(1, 1 + (3000 >> shift));
         const int64_t cap = int64_t(max_pages) << shift;
         const int window = in(0, 2) ? 0x7fffffff : in(1, int(cap) + 5);
         Tables t;
