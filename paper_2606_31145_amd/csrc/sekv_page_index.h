@@ -79,11 +79,11 @@ SEKV_HD int chunk_length(uint64_t W, int T, int max_len, int Hkv, int target, in
     float best = float(max_len);                             // no cut
     if (float(max_len) <= 1.1f * mean) {
         const int rounds = int((all + float(kSlots - 1)) / float(kSlots));
-        float cost = float(rounds) * mean;
+        float cost = float(rounds) * float(max_len);
         for (int k = 1; k <= 4; ++k) {
             const float n = float(int(float(k * kSlots) / all));
-            const float x = n > 1.f ? float(k) * (mean / n + float(over)) : cost;
-            best = x < cost ? mean / n : best;
+            const float x = n > 1.f ? float(k) * (float(max_len) / n + float(over)) : cost;
+            best = x < cost ? float(max_len) / n : best;
             cost = x < cost ? x : cost;
         }
     } else {

@@ -46,6 +46,11 @@ __device__ inline float across16(float x) {
 __device__ inline uint32_t odd2(uint32_t w) { return uint32_t((w & 0x7f80u) == 0x7f80u) | uint32_t((w & 0x7f800000u) == 0x7f800000u); }
 __device__ inline uint32_t odd(const uint4 &v) { return odd2(v.x) | odd2(v.y) | odd2(v.z) | odd2(v.w); }
 __device__ inline bool odd(float x) { return !(fabsf(x) <= 3.402823466e38f); }
+// Is one of four e4m3 codes a NaN.
+__device__ inline uint32_t nan4(uint32_t w) {
+    const uint32_t x = ~w & 0x7f7f7f7fu;               // a zero byte: NaN
+    return (x - 0x01010101u) & ~x & 0x80808080u;
+}
 
 __device__ inline Seq load_seq(const PageAttendArgs &a, int b) {
     const PageTables &t = a.t;
@@ -365,18 +370,6 @@ struct Rows16 {
         }
     }
 
-    // V^T operand of result tile e: bfloat16, 32 keys
-    __device__ static uint4 v_frag(const uint32_t (&vw)[Tile::kBlocks][4][VE / 2], int e) {
-        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                w[2 * j + i] = __builtin_amdgcn_perm(vw[j][2 * i + 1][e / 2], vw[j][2 * i][e / 2], sel);
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-
     // Mask, running maximum and weights of the keys from pos on; valid: a bit for each block that holds
     // keys.  True when some column does not see some key.
     __device__ bool weights(const PageAttendArgs &a, f4v (&s)[J][NB], int pos, uint32_t valid, int lane) {
@@ -435,43 +428,48 @@ struct Rows16 {
     // which some columns do not see holds an infinity or NaN: zero times that is no number.
     __device__ void values(Tile &t, const f4v (&s)[J][NB], int pos, uint32_t valid, bool part, bool *bad, int lane) {
         const int g = lane >> 4;
-        if constexpr (kBf) {
-            uint32_t vw[J][4][VE / 2];
+        if (part) {
 #pragma unroll
             for (int j = 0; j < J; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float sc = P::kBytes == 1 ? pow2_of(t.vs[j] >> (8 * i) & 255u) : 1.f;
+                    const int key = pos + 16 * j + 4 * g + i;
+                    const uint32_t keep = (valid >> j & 1) && key >= lo_any && key <= hi_any ? 0xffffffffu : 0u;
+                    uint32_t wrong = 0;
 #pragma unroll
-                    for (int w = 0; w < VE / 2; ++w) {
-                        if constexpr (P::kBytes == 2) vw[j][i][w] = t.v[j][i][w];
-                        else vw[j][i][w] = codes2_bf16(t.v[j][i][w / 2], sc, w & 1);
+                    for (int w = 0; w < Tile::VW; ++w) {
+                        t.v[j][i][w] &= keep;
+                        wrong |= P::kBytes == 1 ? nan4(t.v[j][i][w]) : P::kBytes == 2 ? odd2(t.v[j][i][w])
+                                                                              : uint32_t(odd(__uint_as_float(t.v[j][i][w])));
                     }
+                    *bad |= wrong != 0;
                 }
-            if (part) {
-#pragma unroll
-                for (int j = 0; j < J; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = pos + 16 * j + 4 * g + i;
-                        const uint32_t keep = (valid >> j & 1) && key >= lo_any && key <= hi_any ? 0xffffffffu : 0u;
-#pragma unroll
-                        for (int w = 0; w < VE / 2; ++w) {
-                            vw[j][i][w] &= keep;
-                            *bad |= odd2(vw[j][i][w]) != 0;
-                        }
-                    }
-            }
+        }
+        if constexpr (kBf) {
             uint4 pf[NB];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
                 pf[nb] = make_uint4(bf16_pack(s[0][nb][0], s[0][nb][1]), bf16_pack(s[0][nb][2], s[0][nb][3]),
                                     bf16_pack(s[J - 1][nb][0], s[J - 1][nb][1]), bf16_pack(s[J - 1][nb][2], s[J - 1][nb][3]));
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const uint4 vf = v_frag(vw, e);
+            for (int w = 0; w < VE / 2; ++w) {
+                uint32_t x[J][4];                             // elements 2 w and 2 w + 1 of the lane's rows
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) o[nb][e] = mma16(vf, pf[nb], o[nb][e]);
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (P::kBytes == 2) x[j][i] = t.v[j][i][w];
+                        else x[j][i] = codes2_bf16(t.v[j][i][w / 2], pow2_of(t.vs[j] >> (8 * i) & 255u), w & 1);
+                    }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t sel = u ? 0x07060302u : 0x05040100u;
+                    const uint4 vf = make_uint4(__builtin_amdgcn_perm(x[0][1], x[0][0], sel), __builtin_amdgcn_perm(x[0][3], x[0][2], sel),
+                                                __builtin_amdgcn_perm(x[J - 1][1], x[J - 1][0], sel),
+                                                __builtin_amdgcn_perm(x[J - 1][3], x[J - 1][2], sel));
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) o[nb][2 * w + u] = mma16(vf, pf[nb], o[nb][2 * w + u]);
+                }
             }
         } else {
 #pragma unroll
@@ -489,15 +487,6 @@ struct Rows16 {
                         for (int u = 0; u < 4; ++u) vf[4 * w + u] = x[u];
                     }
                 }
-                if (part) {
-                    const int key = pos + 4 * g + i;
-                    const bool keep = valid && key >= lo_any && key <= hi_any;
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        vf[e] = keep ? vf[e] : 0.f;
-                        *bad |= odd(vf[e]);
-                    }
-                }
 #pragma unroll
                 for (int e = 0; e < VE; ++e)
 #pragma unroll
@@ -506,31 +495,49 @@ struct Rows16 {
         }
     }
 
-    // Every step-th group of keys from pos on; row blocks are looked up a step ahead, and a step's keys and
-    // values are asked for as soon as the registers of the last ones are free.
+    // Every step-th group of keys from pos on.  A group's keys and values are asked for as soon as the registers
+    // of an earlier one are free, kAhead groups ahead; its row blocks one group before that.
+    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW), kSums = NB * (D / 4 + QW);
+    static constexpr int kAhead = 2 * kTileWords + kSums <= 176 ? 2 : 1;      // of 256 registers
     __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int step, bool *bad, int lane) {
         if (pos >= it.end) return;
-        Tile t;
+        Tile t[kAhead];
+        uint32_t valid[kAhead];
         int row[J];
-        look(a, it, b, g, pos, row, lane);
-        t.load_keys(a, row, lane);
-        t.load_values(a, row, lane);
-        for (;;) {
-            uint32_t valid = 0;
 #pragma unroll
-            for (int j = 0; j < J; ++j) valid |= row[j] >= 0 ? 1u << j : 0u;
-            const int next = pos + step;
-            const bool more = next < it.end;
-            if (more) look(a, it, b, g, next, row, lane);
-            f4v s[J][NB];
-            scores(t, s);
-            if (more) t.load_keys(a, row, lane);
-            const bool part = weights(a, s, pos, valid, lane);
-            values(t, s, pos, valid, part, bad, lane);
-            if (!more) return;
-            t.load_values(a, row, lane);
-            pos = next;
+        for (int u = 0; u < kAhead; ++u) {
+            look(a, it, b, g, pos + u * step, row, lane);
+            valid[u] = bits(row);
+            if (pos + u * step < it.end) {
+                t[u].load_keys(a, row, lane);
+                t[u].load_values(a, row, lane);
+            }
         }
+        for (;;) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int next = pos + kAhead * step;
+                const bool more = next < it.end;
+                if (more) look(a, it, b, g, next, row, lane);
+                f4v s[J][NB];
+                scores(t[u], s);
+                if (more) t[u].load_keys(a, row, lane);
+                const bool part = weights(a, s, pos, valid[u], lane);
+                values(t[u], s, pos, valid[u], part, bad, lane);
+                if (more) {
+                    t[u].load_values(a, row, lane);
+                    valid[u] = bits(row);
+                }
+                pos += step;
+                if (pos >= it.end) return;
+            }
+        }
+    }
+    __device__ static uint32_t bits(const int (&row)[J]) {
+        uint32_t v = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) v |= row[j] >= 0 ? 1u << j : 0u;
+        return v;
     }
     __device__ static void look(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int (&row)[J], int lane) {
 #pragma unroll

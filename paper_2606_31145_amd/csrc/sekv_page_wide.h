@@ -40,12 +40,6 @@ template <int D> struct Swizzle {
     }
 };
 
-// Is one of four e4m3 codes a NaN.
-__device__ inline bool nan4(uint32_t w) {
-    const uint32_t x = ~w & 0x7f7f7f7fu;               // a zero byte: NaN
-    return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
-}
-
 // A wave's 16 rows of keys and values on their way from a page into LDS.
 template <class P, int D>
 struct Stage {
@@ -81,7 +75,7 @@ struct Stage {
                 bad |= odd(make_uint4(v[i].x, v[i].y, v[i].z, v[i].w));
             } else {
                 vs[i] = keep ? vs[i] : 127u;
-                bad |= uint32_t(nan4(v[i].x)) | uint32_t(nan4(v[i].y)) | uint32_t(nan4(v[i].z)) | uint32_t(nan4(v[i].w));
+                bad |= nan4(v[i].x) | nan4(v[i].y) | nan4(v[i].z) | nan4(v[i].w);
             }
         }
         return bad != 0;
