@@ -96,6 +96,17 @@ __device__ inline bool wide_f32(const PageAttendArgs &a, const Item &it, int b, 
     return false;
 }
 
+// One tile's work while the next one's bytes arrive.  The two tiles do not overlap, and saying so keeps the
+// compiler from waiting for the arrival before it reads.
+template <int D>
+__device__ __forceinline__ void step_beside_load(const PageAttendArgs &a, Rows32<D> &r, const Direct<D> &dr, bool more, int next_row,
+                                                 int own, lds_bytes __restrict__ kt, lds_bytes __restrict__ vt,
+                                                 lds_bytes __restrict__ kn, lds_bytes __restrict__ vn, bool rows, int pos,
+                                                 uint32_t valid, bool part, int lane) {
+    if (more) dr.load(a, next_row, kn, vn, own);
+    if (rows) r.step(a, kt, vt, pos, valid, part, lane);
+}
+
 // Up to 128 bfloat16 rows: tiles of 64 keys in LDS, two buffers; a wave fetches 16 keys of each.
 template <class P, int D>
 __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
@@ -104,8 +115,15 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     r.init(a, it, g, wave * 32, lane);
     const int64_t w = it.p0 + it.n_tok - 1 - (int64_t(a.window) - 1);
     const int64_t all_lo = w, all_hi = it.p0;                // keys that every row of the item sees
+    constexpr bool kDirect = P::kBytes == 2;
     Stage<P, D> st;
+    Direct<D> dr;
     bool bad = false;
+    // everybody's part of a tile is in LDS
+    auto arrived = [&]() {
+        if (kDirect) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
     // the four blocks of a tile, one a lane: their page, read two tiles ahead, then mine to fetch and which of
     // them hold keys
     auto page_of = [&](int pos) {
@@ -119,38 +137,50 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
         return uint32_t(__ballot(row >= 0)) & 15u;
     };
     auto partial = [&](int pos, uint32_t valid) { return valid != 15u || pos < all_lo || pos + 63 > all_hi; };
-    auto store = [&](int pos, uint32_t valid, int buf) {
-        if (partial(pos, valid)) bad |= st.mend(wave * 16, valid >> wave & 1 ? it.end - pos : 0, lane);
-        st.store(lds + buf * kTile, lds + (2 + buf) * kTile, wave * 16, lane);
-    };
-    int pos = it.begin;
-    int mine = -1;
-    uint32_t valid = rows_of(pos, page_of(pos), &mine);
-    st.load(a, mine, lane);
-    int page = page_of(pos + 64);
-    uint32_t ahead = 0;
-    store(pos, valid, 0);
-    __syncthreads();
     const lds_bytes tile = (lds_bytes)lds;
+    const int own = wave * 16;
+    auto end_of = [&](int pos, uint32_t valid) { return valid >> wave & 1 ? it.end - pos : 0; };
+    int pos = it.begin, mine = -1;
+    uint32_t valid = rows_of(pos, page_of(pos), &mine), ahead = 0;
+    int page = page_of(pos + 64);
+    if constexpr (kDirect) {
+        dr.init(lane);
+        dr.load(a, mine, tile, tile + 2 * kTile, own);
+    } else {
+        st.load(a, mine, lane);
+        if (partial(pos, valid)) bad |= st.mend(own, end_of(pos, valid), lane);
+        st.store(lds, lds + 2 * kTile, own, lane);
+    }
+    arrived();
     // one tile from buffer kBuf, the next one into the other; false when that was the last
     auto turn = [&](auto kBuf) {
         constexpr int B = decltype(kBuf)::value;
         const bool more = pos + 64 < it.end;
+        if (kDirect && partial(pos, valid)) {
+            bad |= dr.mend(lds + (2 + B) * kTile, own, end_of(pos, valid), lane);
+            __syncthreads();
+        }
+        const bool part = partial(pos, valid), rows = wave * 32 < it.rows;
         if (more) {
             ahead = rows_of(pos + 64, page, &mine);
-            st.load(a, mine, lane);
             page = page_of(pos + 128);
         }
-        if (wave * 32 < it.rows) r.step(a, tile + B * kTile, tile + (2 + B) * kTile, pos, valid, partial(pos, valid), lane);
-        if (more) store(pos + 64, ahead, 1 - B);
-        __syncthreads();
+        if constexpr (kDirect) {
+            step_beside_load<D>(a, r, dr, more, mine, own, tile + B * kTile, tile + (2 + B) * kTile, tile + (1 - B) * kTile,
+                                tile + (3 - B) * kTile, rows, pos, valid, part, lane);
+        } else {
+            if (more) st.load(a, mine, lane);
+            if (rows) r.step(a, tile + B * kTile, tile + (2 + B) * kTile, pos, valid, part, lane);
+            if (more) {
+                if (partial(pos + 64, ahead)) bad |= st.mend(own, end_of(pos + 64, ahead), lane);
+                st.store(lds + (1 - B) * kTile, lds + (3 - B) * kTile, own, lane);
+            }
+        }
+        arrived();
         pos += 64;
         valid = ahead;
         return more;
     };
-    // Two waves share a SIMD, and in step they would want the matrix unit and then the vector unit at the same
-    // time: one goes first, by its slot, and the other fills what it leaves.
-    if (__builtin_amdgcn_s_getreg(6148) & 1) __builtin_amdgcn_s_setprio(1);
     if (it.begin < it.end)
         while (turn(std::integral_constant<int, 0>{}) && turn(std::integral_constant<int, 1>{})) {}
     if (__syncthreads_or(bad)) return true;

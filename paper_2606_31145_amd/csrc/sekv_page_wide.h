@@ -101,6 +101,49 @@ struct Stage {
     }
 };
 
+// The same for bfloat16 storage without a way through registers: each lane names the 16 bytes that belong
+// at its place in the tile, and the memory system writes them there.  Values are mended in the tile.
+template <int D>
+struct Direct {
+    static constexpr int N = D / 32, PC = D / 8;       // pieces a lane; pieces a row
+    int koff[N], voff[N];                              // bytes from the block's first row
+
+    __device__ void init(int lane) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int row = i * (64 / PC) + lane / PC, c = lane % PC;
+            koff[i] = row * (D * 2) + ((c ^ Swizzle<D>::key(row)) << 4);
+            voff[i] = row * (D * 2) + ((c ^ Swizzle<D>::value(row)) << 4);
+        }
+    }
+    // rows of pool row row0 on into the tile's rows row .. row + 15
+    __device__ void load(const PageAttendArgs &a, int row0, lds_bytes kt, lds_bytes vt, int row) const {
+        typedef const __attribute__((address_space(1))) void *global;
+        const size_t r0 = row0 >= 0 ? row0 : 0;        // any row: its keys are masked
+        const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * (D * 2);
+        const unsigned char *vp = static_cast<const unsigned char *>(a.v) + r0 * (D * 2);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            __builtin_amdgcn_global_load_lds((global)(kp + koff[i]), kt + row * (D * 2) + i * 1024, 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global)(vp + voff[i]), vt + row * (D * 2) + i * 1024, 16, 0, 0);
+        }
+    }
+    // as Stage::mend, for the tile's rows row .. row + 15
+    __device__ bool mend(unsigned char *vt, int row, int end, int lane) const {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint4 *p = reinterpret_cast<uint4 *>(vt + row * (D * 2) + i * 1024 + lane * 16);
+            const uint32_t keep = row + i * (64 / PC) + lane / PC >= end ? 0u : ~0u;
+            uint4 w = *p;
+            w = make_uint4(w.x & keep, w.y & keep, w.z & keep, w.w & keep);
+            *p = w;
+            bad |= odd(w);
+        }
+        return bad != 0;
+    }
+};
+
 template <int D>
 struct Rows32 {
     static constexpr int DB = D / 32, QS = D / 16;
