@@ -20,6 +20,7 @@ namespace {
 using namespace page;
 
 constexpr int kThreads = 256, kWaves = 4;
+constexpr int64_t kJoinBlocks = 2048;      // eight on each compute unit
 
 // At most 16 NB rows: every wave takes all of them, and every fourth step of the keys.  True when the
 // item has to be done again by plain_rows.
@@ -238,10 +239,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
     join_rows<T, D, true>(a, it, g, 0, it.rows, lane, lds);
 }
 
-// Joins the partials of 16 rows of a tile at a time.
+// Joins the partials of as many rows of a tile at a time as a workgroup holds side by side.
+constexpr int join_parts(int D) { return kTileRows / (kThreads / (D / 4)); }
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
-    constexpr int kRows = 16, kParts = kTileRows / kRows;
+    constexpr int kParts = join_parts(D), kRows = kTileRows / kParts;
     __shared__ __attribute__((aligned(16))) unsigned char lds[256 * (sizeof(float4) + sizeof(float2))];
     const int lane = threadIdx.x & 63;
     const Plan plan = make_plan(a, lane);
@@ -269,8 +271,8 @@ hipError_t SEKV_NAME(SEKV_T, SEKV_P, SEKV_D)(const PageAttendArgs &a, hipStream_
     hipLaunchKernelGGL((attend_kernel<T, P, SEKV_D>), dim3(unsigned(page::blocks_of(a.pairs, a.t.Hkv))), dim3(kThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1 || !a.join_launch) return e;
-    const int64_t parts = a.tiles * a.t.Hkv * (page::kTileRows / 16);
-    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned(parts < 1024 ? parts : 1024)), dim3(kThreads), 0, s, a);
+    const int64_t parts = a.tiles * a.t.Hkv * join_parts(SEKV_D);
+    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned(parts < kJoinBlocks ? parts : kJoinBlocks)), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -34,7 +34,7 @@ constexpr int kFewRows = 64;       // rows of two narrow tiles, which read the k
 constexpr int kTileRows = 128;     // 32 rows for each of four waves
 constexpr int kChunkStep = 128;    // keys: a step of 32 for each of four waves
 constexpr int kSlots = 512;        // workgroups that run at once: two on each of 256 compute units
-constexpr int kOverNarrow = 128, kOverWide = 512;    // keys that an item costs beside its own
+constexpr int kOverNarrow = 128, kOverWide = 1024;    // keys that an item costs beside its own
 constexpr int kBlock = 16;         // keys that lie in one page: the smallest page
 
 // Pool row of position `pos` (below max_pages * page_size) from its table entry; -1 when the page is
