@@ -32,7 +32,7 @@ namespace page {
 constexpr int kNarrowRows = 32;    // one or two 16-wide matrix tiles
 constexpr int kFewRows = 64;       // rows of two narrow tiles, which read the keys twice, the second time from cache
 constexpr int kTileRows = 128;     // 32 rows for each of four waves
-constexpr int kChunkStep = 128;    // keys: a step of 32 for each of four waves
+constexpr int kChunkStep = 64;     // keys: a tile of the wide form, one or two steps of four waves in the narrow one
 constexpr int kSlots = 512;        // workgroups that run at once: two on each of 256 compute units
 constexpr int kOverNarrow = 128, kOverWide = 1024;    // keys that an item costs beside its own
 constexpr int kBlock = 16;         // keys that lie in one page: the smallest page
