@@ -342,11 +342,12 @@ SEKV_API sekv_status sekv_build_cache(const sekv_build_dims *dims, const void *k
  *   the row's finite values, at least 1; E = 127 for a row without finite non-zero values.
  * The scale is a power of two, so scaling is exact and a stored value is off by at most half
  * an e4m3 step (2^-4 of it, or 2^-10 * 2^(E - 127) for the smallest); read back in dims.dtype
- * it is exact again.  Infinities and NaN are stored as NaN in 8 bits.
+ * it is exact again (but for values beyond that type: those that were rounded up past its largest,
+ * and subnormal ones).  Infinities and NaN are stored as NaN in 8 bits.
  *
  * Ragged batches: the new tokens of all sequences lie one after another; sequence b has rows
  * tok_start[b] .. tok_start[b + 1] - 1 of n_tokens (tok_start int32 [B + 1], ascending from 0;
- * rows at tok_start[B] and behind are neither read nor written).  seq_len[b] counts the
+ * rows at tok_start[B] and behind belong to nobody and no output row of theirs is written).  seq_len[b] counts the
  * sequence's tokens with the new ones, so new token i of n_new stands at position
  * seq_len[b] - n_new + i.  Both tables are read on the device: a captured graph may be
  * replayed with other contents.
@@ -363,15 +364,15 @@ typedef struct {
     int32_t n_q_heads;      /* Hq; query head h reads KV head h / (Hq / Hkv)               */
     int32_t n_kv_heads;     /* Hkv; Hq / Hkv in {1, 2, 4, 8}                               */
     int32_t head_dim;       /* d in {64, 128}                                              */
-    int32_t page_size;      /* tokens a page: a power of two, 16..1024 (16 keys fill a     
-                               matrix tile's side)                                         */
+    int32_t page_size;      /* tokens a page: a power of two, 16..1024 (16 keys fill one
+                               side of a matrix tile)                                      */
     int32_t n_pages;        /* pages in the pool, n_pages * Hkv * page_size < 2^31         */
     int32_t max_pages;      /* row stride of the page table, max_pages * page_size <= 2^30 */
     int32_t dtype;          /* SEKV_F32 or SEKV_BF16: new tokens, queries, outputs          */
     int32_t page_dtype;     /* dtype, or SEKV_E4M3                                         */
     int32_t window;         /* a query sees at most this many keys, its own last; 0: all   */
     int32_t reserved[2];    /* 0                                                           */
-    double softmax_scale;
+    double softmax_scale;   /* in [1e-30, 1e30]                                            */
 } sekv_page_dims;
 
 /* One layer's pages.  Device pointers, caller-owned; pools and scales 16-byte aligned. */
@@ -390,7 +391,10 @@ SEKV_API sekv_status sekv_check_page_dims(const sekv_page_dims *dims);
 /* Bytes of device workspace the calls below need for up to n_tokens new tokens (0 if dims are
  * invalid).  Initialise it once with sekv_workspace_init; its error word is read with
  * sekv_workspace_status.  sekv_page_append and sekv_page_read use the error word only (256
- * bytes are enough for them). */
+ * bytes are enough for them).  sekv_page_attend keeps counters in it that it leaves zero:
+ * calls that share a workspace are ordered on one stream, and page calls recorded into a
+ * captured graph do not share one with the step calls (eagerly they may: the library zeroes
+ * what the other kind left). */
 SEKV_API size_t sekv_page_workspace_size(const sekv_page_dims *dims, int32_t n_tokens);
 
 /* Store the new tokens: k, v [n_tokens][Hkv][d] in dims.dtype, consecutive tokens k_stride and
@@ -412,8 +416,8 @@ SEKV_API sekv_status sekv_page_read(const sekv_page_dims *dims, const sekv_pages
  * query at position p sees the keys max(0, p - window + 1) .. p of its sequence (their rows
  * have to be stored before, in stream order).  Writes out [n_tokens][Hq][d] in dims.dtype and,
  * unless NULL, lse float [n_tokens][Hq], the natural logarithm of the softmax's denominator.
- * A query that sees nothing (position below 0) gets zeros and -inf.  Keys and values that a
- * query does not see do not reach it, whatever they hold.
+ * A query that sees nothing (position below 0), or whose scores are all -inf, gets zeros and
+ * -inf.  Keys and values that a query does not see do not reach it, whatever they hold.
  * Scores and sums are held in float; with bfloat16 tokens the softmax weights are rounded to
  * bfloat16 for the matrix cores (off by at most 2^-8 of each); with float tokens nothing is. */
 SEKV_API sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages, const void *q,

@@ -332,6 +332,8 @@ sekv_status check_page_dims(const sekv_page_dims *d) {
         return fail(SEKV_ERR_INVALID_ARG, "reserved field is not 0");
     if (!(d->softmax_scale > 0.0) || !std::isfinite(d->softmax_scale))
         return fail(SEKV_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    if (d->softmax_scale < 1e-30 || d->softmax_scale > 1e30)
+        return fail(SEKV_ERR_UNSUPPORTED, "softmax_scale %g outside [1e-30, 1e30]", d->softmax_scale);
     return SEKV_OK;
 }
 

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from tests.gpu_common import banner
-from tests.page_common import TORCH, Case, encode_rows
+from tests.page_common import TORCH, Case, decode_rows, encode_rows
 
 pytestmark = pytest.mark.gpu
 
@@ -172,6 +172,20 @@ def test_read(S, dtype, store, kw):
     assert ws.status() == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_read_scales_over_the_range(S, dtype):
+    c = Case(dtype, "e4m3", [64], [0], dim=128, page=32)
+    g = torch.Generator().manual_seed(1)
+    for name in "kv":
+        codes, e = c.codes[name]
+        e.copy_(torch.randint(20, 240, e.shape, generator=g).to(torch.uint8))
+        c.pools[name] = decode_rows(codes, e)
+    keys, values = S.page_read(c.dims(S), c.cache(S), 64, c.workspace(S))
+    for got, name in ((keys, "k"), (values, "v")):
+        for h in range(c.Hkv):
+            assert torch.equal(got[0, h].cpu().double(), c.dense(name, 0, h)[0])
+
+
 def test_read_skips_bad_pages(S):
     c = Case("bf16", "e4m3", [40, 20], [0, 0])
     c.table[0, 1], c.table[1, 0] = c.n_pages, -5
@@ -229,6 +243,10 @@ ATTENDS = [
     dict(lens=[2500, 31], news=[20, 31], group=4, kv_heads=1, dim=64, page=16, strided=True),
     dict(lens=[40, 30], news=[3, 30], group=2, page=16),
     dict(lens=[70, 41], news=[1, 37], group=4, dim=128, spread=8.0),       # weights of one entry almost
+    dict(lens=[2000] + [30] * 7, news=[40] + [1] * 7, group=4, kv_heads=1, dim=128),   # one wide tile among narrow ones
+    dict(lens=[3000], news=[4], group=4, kv_heads=4, page=1024, dim=64),
+    dict(lens=[1500, 1400], news=[12, 3], group=4, kv_heads=1, dim=128, page=64, window=700),
+    dict(lens=[900, 64], news=[64, 64], group=1, kv_heads=4, dim=128, page=32),
 ]
 
 

@@ -36,7 +36,8 @@ def _dims(S, **kw):
     (dict(page_size=2048), 2), (dict(n_pages=0), 1), (dict(max_pages=0), 1), (dict(n_pages=1 << 27), 2),
     (dict(max_pages=(1 << 26) + 1), 2), (dict(dtype=2), 2), (dict(dtype="bf16", page_dtype="f32"), 2),
     (dict(dtype="f32", page_dtype="bf16"), 2), (dict(window=-1), 1), (dict(softmax_scale=0.0), 1),
-    (dict(softmax_scale=float("nan")), 1), (dict(softmax_scale=float("inf")), 1),
+    (dict(softmax_scale=float("nan")), 1), (dict(softmax_scale=float("inf")), 1), (dict(softmax_scale=1e-40), 2),
+    (dict(softmax_scale=1e40), 2),
 ])
 def test_bad_dims_are_refused(S, kw, status):
     d = _dims(S, **kw)
@@ -55,7 +56,7 @@ def test_reserved_fields_and_counts_are_refused(S):
     with pytest.raises(S.SekvError):
         S.page_workspace_size(_dims(S), -1)
     with pytest.raises(S.SekvError):
-        S.check_page_dims(None) if False else S._check(S.LIB.sekv_check_page_dims(None))
+        S._check(S.LIB.sekv_check_page_dims(None))
 
 
 @pytest.mark.parametrize("kw", [dict(), dict(dtype="f32"), dict(page_dtype="e4m3"), dict(batch=0),
