@@ -76,11 +76,15 @@ SEKV_HD Seq make_seq(int start, int end, int seq_len, int n_tokens, int64_t cap,
     return s;
 }
 
+// A 64-bit quotient costs a wave some 150 instructions, a 32-bit one a fifth: every workgroup starts with
+// these.
+SEKV_HD uint64_t quotient(uint64_t a, uint32_t b) { return a >> 32 ? a / b : uint64_t(uint32_t(a) / b); }
+
 // W, T: of one KV head
 SEKV_HD int chunk_length(uint64_t W, int T, int max_len, int Hkv, int target, int splits, int over) {
     if (T < 1) return kChunkStep;
-    uint64_t c = (W + target - 1) / uint64_t(target);
-    const uint64_t d = (uint64_t(max_len) + splits - 1) / uint64_t(splits);
+    uint64_t c = quotient(W + target - 1, uint32_t(target));
+    const uint32_t d = (uint32_t(max_len) + uint32_t(splits) - 1) / uint32_t(splits);
     c = c > d ? c : d;
     const float mean = float(W) / float(T), all = float(T) * float(Hkv);
     float best = float(max_len);                             // no cut
@@ -97,10 +101,10 @@ SEKV_HD int chunk_length(uint64_t W, int T, int max_len, int Hkv, int target, in
         const float x = sqrtf(mean * all * float(over) / float(kSlots));
         best = x < best ? x : best;
     }
-    const uint64_t m = uint64_t(best) + 1;
+    const uint32_t m = uint32_t(best) + 1;
     c = c > m ? c : m;
-    c = (c + kChunkStep - 1) / kChunkStep * kChunkStep;
-    return int(c > (1u << 30) ? (1u << 30) : c);
+    const uint32_t r = uint32_t(c > (1u << 30) ? (1u << 30) : c);
+    return int((r + kChunkStep - 1) / kChunkStep * kChunkStep);
 }
 SEKV_HD int chunks_of(const Seq &s, int chunk) { return s.len > chunk ? (s.len + chunk - 1) / chunk : 1; }
 
@@ -124,19 +128,18 @@ SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, in
     it.n_tok = left < per ? left : per;
     it.rows = it.n_tok << group_shift;
     it.p0 = s.first + t0;
-    int64_t b = it.p0 - (int64_t(window) - 1), e = it.p0 + it.n_tok;
-    b = b < 0 ? 0 : b / 64 * 64;
-    e = e < 0 ? 0 : e < cap ? e : cap;
-    if (b >= e) {                                  // no key: the first chunk's item says so
-        it.begin = it.end = 0;
-        it.chunk0 = it.chunk1 = 0;
-        it.idle = c != 0;
-        return it;
-    }
-    it.chunk0 = int((b - s.lo) / chunk);
-    it.chunk1 = int((e - 1 - s.lo) / chunk);
+    const int64_t b64 = it.p0 - (int64_t(window) - 1), e64 = it.p0 + it.n_tok;
+    const uint32_t b = b64 < 0 ? 0u : b64 < cap ? uint32_t(b64) & ~63u : uint32_t(cap);
+    const uint32_t e = e64 < 0 ? 0u : e64 < cap ? uint32_t(e64) : uint32_t(cap);
+    it.begin = it.end = 0;
+    it.chunk0 = it.chunk1 = 0;
+    it.idle = c != 0;
+    if (b >= e) return it;                         // no key: the first chunk's item says so
+    it.chunk0 = int((b - uint32_t(s.lo)) / uint32_t(chunk));
+    it.chunk1 = int((e - 1 - uint32_t(s.lo)) / uint32_t(chunk));
     it.idle = c < it.chunk0 || c > it.chunk1;
-    const int64_t cb = s.lo + int64_t(c) * chunk, ce = cb + chunk;
+    if (it.idle) return it;
+    const uint32_t cb = uint32_t(s.lo) + uint32_t(c) * uint32_t(chunk), ce = cb + uint32_t(chunk);    // below 2^31
     it.begin = int(b > cb ? b : cb);
     it.end = int(e < ce ? e : ce);
     return it;
