@@ -65,9 +65,12 @@ sekv::PageTables tables(const sekv_page_dims *d, const sekv_pages *p, const int3
     return t;
 }
 
-// Work items that fill the device: two workgroups a compute unit, four rounds of them, so that
-// ragged chunks even out.
-constexpr int kItems = 2048;
+// Work items aimed at: two workgroups a compute unit, two rounds of them, so that ragged chunks even out.
+// A workgroup without an item still has to be started and to find that out.  Measured (us) with 512, 1024
+// and 2048: one token of 8 sequences at 9000 in 8 bits 30.6, 30.5, 34.0; six of 16 under a window 30.8,
+// 30.9, 32.8; one of 32 ragged sequences of up to 32768 in bfloat16 511, 465, 453; one of 5 of up to 131072
+// in 8 bits 218, 188, 191; 9 ragged ones, one of 300 tokens, 467, 425, 434.
+constexpr int kItems = 1024;
 
 sekv::page::Launch plan(const sekv_page_dims *d, int n_tokens) {
     return sekv::page::plan_launch(d->batch, n_tokens, d->n_kv_heads, log2_of(d->n_q_heads / d->n_kv_heads),
