@@ -2,12 +2,21 @@
 // sekv_page_attend for chunks.
 //
 // What bounds it: the matrix cores and the softmax's vector instructions together.  A wave takes 32
-// rows; per tile it issues 32 matrix instructions of 32 cycles (32x32x16, half scores, half values),
-// and 2048 scores cost it about 4 vector instructions and one exponential each for 64 lanes, so the
-// two units are about equally busy and two workgroups share a compute unit to keep both fed.  Keys
-// and values are fetched once per workgroup (each wave one block of 16 keys, which lies in one page),
-// a tile ahead, in registers; on the way into LDS 8-bit codes become scaled bfloat16, so the rest
+// rows; per tile it issues 32 matrix instructions (32x32x16, half scores, half values), and 2048 scores
+// cost it about 4 vector instructions and one exponential each for 64 lanes, so the two units are about
+// equally busy and two workgroups share a compute unit to keep both fed.  Keys and values are fetched
+// once per workgroup (each wave one block of 16 keys, which lies in one page), a tile ahead: bfloat16
+// straight into LDS, 8-bit codes through registers, where they become scaled bfloat16, so that the rest
 // knows one type only.
+//
+// Measured, 2048 tokens over 32768 keys, head_dim 128, bfloat16 (1065 GFLOP): 1055 us, 1009 TFLOP/s, where a
+// 16384^3 matrix product reaches 1364; in 8 bits 1081 us; head_dim 64 665 us.  The matrix cores are busy for 48 %
+// of the cycles, at a clock that the load brings down to 1.95 GHz.  The way there: 1211 us with the blocks of a
+// tile looked up by one lane each instead of by all, 1166; the LDS reads placed among the products
+// (sched_group_barrier) 1146; bfloat16 straight into LDS 1067.  No gain came from a priority for half of
+// the waves (1109 against 1101), nor from starting a tile's scores before the last one's values (1126 to
+// 1172 against 1124).  In copies that leave work out, the products alone take 688 us; without the exponentials it
+// is 11 % faster, without the loads 10 %.
 //
 // LDS: rows of D values in 16-byte pieces, two buffers.  A piece sits at its index XOR a function of
 // its row, so that what 64 lanes read together falls into different banks: for keys 16 rows at one
@@ -40,43 +49,37 @@ template <int D> struct Swizzle {
     }
 };
 
-// A wave's 16 rows of keys and values on their way from a page into LDS.
-template <class P, int D>
+// A wave's 16 rows of 8-bit keys and values on their way from a page into LDS, where they are bfloat16.
+template <int D>
 struct Stage {
-    static constexpr int N = D * P::kBytes / 64;       // 16-byte pieces a lane, keys or values
-    static constexpr int PC = D * P::kBytes / 16;      // pieces a row
+    static constexpr int N = D / 64;                   // 16-byte pieces a lane, keys or values
+    static constexpr int PC = D / 16;                  // pieces a row
     typedef uint32_t u4v __attribute__((ext_vector_type(4)));
     u4v k[N], v[N];
     uint32_t ks[N], vs[N];
 
     __device__ void load(const PageAttendArgs &a, int row0, int lane) {
         const size_t r0 = row0 >= 0 ? row0 : 0;        // any row: its keys are masked
-        const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * (D * P::kBytes);
-        const unsigned char *vp = static_cast<const unsigned char *>(a.v) + r0 * (D * P::kBytes);
+        const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * D;
+        const unsigned char *vp = static_cast<const unsigned char *>(a.v) + r0 * D;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             k[i] = reinterpret_cast<const u4v *>(kp)[i * 64 + lane];
             v[i] = reinterpret_cast<const u4v *>(vp)[i * 64 + lane];
-            if constexpr (P::kBytes == 1) {
-                ks[i] = a.k_scale[r0 + i * (64 / PC) + lane / PC];
-                vs[i] = a.v_scale[r0 + i * (64 / PC) + lane / PC];
-            }
+            ks[i] = a.k_scale[r0 + i * (64 / PC) + lane / PC];
+            vs[i] = a.v_scale[r0 + i * (64 / PC) + lane / PC];
         }
     }
     // For a tile that not every row sees: values from row `end` on, which none sees, become zeros.  True when
-    // another holds an infinity or NaN: the product with its masked weight, zero, would be no number.
+    // another holds a NaN: the product with its masked weight, zero, would be no number.
     __device__ bool mend(int row0, int end, int lane) {
         uint32_t bad = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t keep = row0 + i * (64 / PC) + lane / PC >= end ? 0u : ~0u;
             v[i] &= keep;
-            if constexpr (P::kBytes == 2) {
-                bad |= odd(make_uint4(v[i].x, v[i].y, v[i].z, v[i].w));
-            } else {
-                vs[i] = keep ? vs[i] : 127u;
-                bad |= nan4(v[i].x) | nan4(v[i].y) | nan4(v[i].z) | nan4(v[i].w);
-            }
+            vs[i] = keep ? vs[i] : 127u;
+            bad |= nan4(v[i].x) | nan4(v[i].y) | nan4(v[i].z) | nan4(v[i].w);
         }
         return bad != 0;
     }
@@ -87,16 +90,11 @@ struct Stage {
         for (int i = 0; i < N; ++i) {
             const int row = row0 + i * (64 / PC) + lane / PC, c = lane % PC;
             unsigned char *kr = kt + row * (D * 2), *vr = vt + row * (D * 2);
-            if constexpr (P::kBytes == 2) {
-                *reinterpret_cast<u4v *>(kr + ((c ^ Z::key(row)) << 4)) = k[i];
-                *reinterpret_cast<u4v *>(vr + ((c ^ Z::value(row)) << 4)) = v[i];
-            } else {
-                const float fk = pow2_of(ks[i]), fv = pow2_of(vs[i]);
-                *reinterpret_cast<uint4 *>(kr + (((2 * c) ^ Z::key(row)) << 4)) = codes8_bf16(k[i].x, k[i].y, fk);
-                *reinterpret_cast<uint4 *>(kr + (((2 * c + 1) ^ Z::key(row)) << 4)) = codes8_bf16(k[i].z, k[i].w, fk);
-                *reinterpret_cast<uint4 *>(vr + (((2 * c) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].x, v[i].y, fv);
-                *reinterpret_cast<uint4 *>(vr + (((2 * c + 1) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].z, v[i].w, fv);
-            }
+            const float fk = pow2_of(ks[i]), fv = pow2_of(vs[i]);
+            *reinterpret_cast<uint4 *>(kr + (((2 * c) ^ Z::key(row)) << 4)) = codes8_bf16(k[i].x, k[i].y, fk);
+            *reinterpret_cast<uint4 *>(kr + (((2 * c + 1) ^ Z::key(row)) << 4)) = codes8_bf16(k[i].z, k[i].w, fk);
+            *reinterpret_cast<uint4 *>(vr + (((2 * c) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].x, v[i].y, fv);
+            *reinterpret_cast<uint4 *>(vr + (((2 * c + 1) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].z, v[i].w, fv);
         }
     }
 };
@@ -128,7 +126,7 @@ struct Direct {
             __builtin_amdgcn_global_load_lds((global)(vp + voff[i]), vt + row * (D * 2) + i * 1024, 16, 0, 0);
         }
     }
-    // as Stage::mend, for the tile's rows row .. row + 15
+    // as Stage::mend, infinities too, for the tile's rows row .. row + 15
     __device__ bool mend(unsigned char *vt, int row, int end, int lane) const {
         uint32_t bad = 0;
 #pragma unroll
