@@ -183,8 +183,8 @@ void ws_note_zeroed(void *ws, size_t bytes) {
 namespace sekv {
 hipError_t ws_prepare_pages(void *ws, size_t bytes, size_t words, hipStream_t stream) {
     std::lock_guard<std::mutex> lk(g_ws_mu);
-    // the counters are all that has to be zero, and their number is all that their place depends on
-    if (g_ws.before_launch(reinterpret_cast<uintptr_t>(ws), bytes, (uint64_t(0x5047) << 48) | words, 1))
+    // the counters are all that has to be zero, and they lie in the same place whatever the call
+    if (g_ws.before_launch(reinterpret_cast<uintptr_t>(ws), bytes, uint64_t(0x5047) << 48, 1))
         return launch_zero_words(static_cast<unsigned char *>(ws) + sizeof(WsHeader), words, stream);
     return hipSuccess;
 }

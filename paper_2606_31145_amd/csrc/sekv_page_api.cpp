@@ -77,15 +77,11 @@ sekv::page::Launch plan(const sekv_page_dims *d, int n_tokens) {
                                    int64_t(d->max_pages) * d->page_size, kItems);
 }
 
-int group_shift(const sekv_page_dims *d) { return log2_of(d->n_q_heads / d->n_kv_heads); }
-size_t counters(const sekv_page_dims *d) {
-    return (size_t(sekv::page::counter_words(d->n_kv_heads, group_shift(d), kItems)) + 63) / 64 * 64;
-}
 // The header, the counters, then the partials of split tiles.
 size_t workspace_bytes(const sekv_page_dims *d, int32_t n_tokens) {
-    const int64_t rows = sekv::page::partial_rows(n_tokens, d->n_kv_heads, group_shift(d),
+    const int64_t rows = sekv::page::partial_rows(n_tokens, d->n_kv_heads, log2_of(d->n_q_heads / d->n_kv_heads),
                                                   int64_t(d->max_pages) * d->page_size, kItems);
-    return sizeof(sekv::WsHeader) + counters(d) * sizeof(uint32_t) + size_t(rows) * (d->head_dim + 2) * sizeof(float);
+    return sizeof(sekv::WsHeader) + sekv::page::kCounters * sizeof(uint32_t) + size_t(rows) * (d->head_dim + 2) * sizeof(float);
 }
 
 }  // namespace
@@ -176,11 +172,11 @@ sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages
     a.splits = l.splits; a.target = l.target; a.tiles = l.tiles; a.pairs = l.pairs;
     a.join_launch = sekv::page::join_in_launch(dims->batch, n_tokens, a.group_shift);
     a.arrived = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(ws) + sizeof(sekv::WsHeader));
-    a.part_o = reinterpret_cast<float *>(a.arrived + counters(dims));
+    a.part_o = reinterpret_cast<float *>(a.arrived + sekv::page::kCounters);
     a.part_ml = a.part_o + size_t(l.splits) * n_tokens * dims->n_q_heads * dims->head_dim;
     if (sekv::page::blocks_of(l.pairs, dims->n_kv_heads) > (int64_t(1) << 23))
         return fail(SEKV_ERR_UNSUPPORTED, "%d new tokens of %d heads in one call", n_tokens, dims->n_q_heads);
-    hipError_t e = l.splits > 1 ? sekv::ws_prepare_pages(ws, ws_bytes, counters(dims), stream) : hipSuccess;
+    hipError_t e = l.splits > 1 ? sekv::ws_prepare_pages(ws, ws_bytes, sekv::page::kCounters, stream) : hipSuccess;
     if (e != hipSuccess) return fail(SEKV_ERR_HIP, "workspace zero kernel: %s", hipGetErrorString(e));
     e = sekv::launch_page_attend(a, dims->dtype, dims->page_dtype, dims->head_dim, stream);
     if (e != hipSuccess) return fail(SEKV_ERR_HIP, "page attention launch: %s", hipGetErrorString(e));

@@ -165,6 +165,10 @@ SEKV_HD int most_splits(int64_t cap) {
     const int64_t n = (cap + kChunkStep - 1) / kChunkStep;
     return int(n > 256 ? 256 : n);
 }
+// Counters of a workspace, [n_tokens][Hkv].  The same for all dims, so that calls of any shape, captured ones
+// among them, keep them in one place that no call's partials reach.  More tokens than that are about as many tiles
+// as fill the device: they are not cut.
+constexpr int kCounters = 1 << 17;
 // `items`: how many work items fill the device.
 SEKV_HD Launch plan_launch(int batch, int n_tokens, int Hkv, int group_shift, int64_t cap, int items) {
     Launch l;
@@ -172,7 +176,7 @@ SEKV_HD Launch plan_launch(int batch, int n_tokens, int Hkv, int group_shift, in
     l.target = (items + Hkv - 1) / Hkv;
     const int64_t s = (int64_t(l.target) * kTileRows + r - 1) / r;
     const int most = most_splits(cap);
-    l.splits = int(s < most ? s : most);
+    l.splits = int64_t(n_tokens) * Hkv > kCounters ? 1 : int(s < most ? s : most);
     l.tiles = most_tiles(batch, n_tokens, group_shift);
     l.pairs = l.tiles + (l.splits > 1 ? l.target : 0);
     return l;
@@ -185,12 +189,6 @@ SEKV_HD int64_t partial_rows(int n_tokens, int Hkv, int group_shift, int64_t cap
     return (a < b ? a : b) * Hkv;
 }
 
-// Counters that any call of these dims needs, [n_tokens][Hkv]: only calls with splits > 1 have any, and
-// those have rows < target * kTileRows.  A number of the dims alone, so that calls of all sizes keep them
-// in the same place.
-SEKV_HD int64_t counter_words(int Hkv, int group_shift, int items) {
-    return (int64_t((items + Hkv - 1) / Hkv) * kTileRows >> group_shift) * Hkv;
-}
 // Whether the partials go to a second kernel.  Joining in the last workgroup of a tile saves a launch but
 // leaves a tile of 128 rows to one compute unit, so it is for tiles that are probably narrow; more rows
 // than sequences of narrow tiles hold mean that some tile is not.  Measured (us), joined in the last workgroup

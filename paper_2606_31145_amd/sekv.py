@@ -814,6 +814,8 @@ def _on(device, stream):
         return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device), st
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the pages on {device}")
     return torch.cuda.stream(stream), stream.cuda_stream
 
 

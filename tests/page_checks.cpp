@@ -26,7 +26,7 @@ static void walk(const Tables &t, int Hkv, int gs, int64_t cap, int window, int 
     REQUIRE(l.splits >= 1 && l.splits <= 256 && l.target >= 1);
     REQUIRE((int64_t(t.n_tokens) << gs) * Hkv * l.splits <= partial_rows(t.n_tokens, Hkv, gs, cap, items));
     REQUIRE(partial_rows(t.n_tokens, Hkv, gs, cap, items) <= partial_rows(t.n_tokens + 1, Hkv, gs, cap, items));
-    if (l.splits > 1) REQUIRE(int64_t(t.n_tokens) * Hkv <= counter_words(Hkv, gs, items));
+    if (l.splits > 1) REQUIRE(int64_t(t.n_tokens) * Hkv <= kCounters);
     if (good) {                                          // every (pair, head) is some workgroup's, once
         const int64_t n = blocks_of(l.pairs, Hkv);
         std::vector<int> got(size_t(n) , 0);

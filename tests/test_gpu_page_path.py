@@ -162,6 +162,35 @@ def test_captured_calls_follow_the_tables(S, store):
     assert ws.status() == 0
 
 
+def test_graphs_of_different_shapes_share_a_workspace(S):
+    """Captured calls of other head counts and types in turn on one workspace: each finds its counters zero."""
+    banner("graphs of shapes")
+    cases = [Case("bf16", "e4m3", [3000, 900], [1, 2], dim=128, kv_heads=2, group=8, page=16, seed=1),
+             Case("f32", "same", [1500], [1], dim=64, kv_heads=7, group=1, page=16, seed=2),
+             Case("bf16", "same", [700, 2600], [150, 300], dim=64, kv_heads=3, group=2, page=32, seed=3)]
+    ws = S.Workspace(None, "cuda", nbytes=max(S.page_workspace_size(c.dims(S), sum(c.news)) for c in cases))
+    parts = []
+    for c in cases:
+        cache, q, ts = c.cache(S), c.q.cuda(), c.tok_start()
+        own = c.workspace(S)
+        want = S.page_attend(c.dims(S), cache, q, ts, own, want_lse=True)
+        out, lse = torch.empty_like(want[0]), torch.empty_like(want[1])
+        S.page_attend(c.dims(S), cache, q, ts, ws, out=out, lse=lse)
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            S.page_attend(c.dims(S), cache, q, ts, ws, out=out, lse=lse)
+        parts.append((gr, cache, q, ts, out, lse, want, own))
+    for turn in (0, 1, 2, 1, 0, 2, 2, 0):
+        gr, cache, q, ts, out, lse, want, own = parts[turn]
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        gr.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]), turn
+    assert ws.status() == 0
+
+
 def test_wrong_tables_leave_nothing_behind(S):
     """tok_start that descends or passes n_tokens, and a negative or too long seq_len: flagged, and the next
     call on the workspace is right."""
