@@ -220,11 +220,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
                 (s.nq && a.t.seq_len[b] > cap))
                 flag(a.t);
         }
-    const Plan plan = make_plan(a, lane);
+    const Plan plan = make_plan(a, lane, lds);
     int b = 0, c = 0, g = 0;
     const uint32_t x = place_of(blockIdx.x, a.t.Hkv, &g);
     Item it;
-    if (!plan.chunk || !find_item(a, x, lane, plan, &b, &c, &it)) return;
+    if (!plan.chunk || !find_item(a, x, lane, plan, lds, &b, &c, &it)) return;
     bool again;
     if (it.narrow && it.rows <= 16) again = narrow<T, P, D, 1>(a, it, b, g, c, lane, wave, lds);
     else if (it.narrow) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);
@@ -253,14 +253,14 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
     constexpr int kParts = join_parts(D), kRows = kTileRows / kParts;
     __shared__ __attribute__((aligned(16))) unsigned char lds[256 * (sizeof(float4) + sizeof(float2))];
     const int lane = threadIdx.x & 63;
-    const Plan plan = make_plan(a, lane);
+    const Plan plan = make_plan(a, lane, lds);
     if (!plan.chunk || plan.longest <= plan.chunk) return;   // nothing was cut
     const int64_t all = int64_t(plan.tiles) * a.t.Hkv * kParts;
     for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
         const int g = int(u % a.t.Hkv), part = int(u / a.t.Hkv % kParts);
         int b = 0, c = 0;
         Item it;
-        find_item<true>(a, uint32_t(u / a.t.Hkv / kParts), lane, plan, &b, &c, &it);
+        find_item<true>(a, uint32_t(u / a.t.Hkv / kParts), lane, plan, lds, &b, &c, &it);
         const int left = it.rows - part * kRows;
         if (it.chunk0 == it.chunk1 || left <= 0) continue;
         join_rows<T, D, false>(a, it, g, part * kRows, left < kRows ? left : kRows, lane, lds);

@@ -72,33 +72,41 @@ __device__ inline Seq of_lane(const Seq &s, int l) {
     return r;
 }
 
-// What every wave finds out about the call for itself.
+// What a workgroup finds out about the call.  Up to 64 sequences are one a lane, and every wave does it for itself;
+// of more, a thread takes B / 256 consecutive ones, twice, and the threads meet in LDS (4096 sequences of 300
+// tokens 873 us, with 64 at a time in every wave 2011).
 struct Plan {
-    Seq mine;             // sequence `lane`: the tables of up to 64 sequences are read once
+    Seq mine;             // sequence `lane` of up to 64
     int chunk;            // 0 where tok_start does not ascend within the new tokens: rows could then belong to
                           // two sequences, and a tile's counter to two tiles
     int tiles, longest;   // of a KV head; keys of the longest sequence (where chunks may be cut)
 };
 
-__device__ inline Plan make_plan(const PageAttendArgs &a, int lane) {
+// lds: 256 bytes, free again on return.
+__device__ inline Plan make_plan(const PageAttendArgs &a, int lane, unsigned char *lds) {
     Plan p;
     uint64_t W = 0;
     int mx = 0, T = 0;
     bool wrong = false;
-    for (int b = lane; b < a.t.B; b += 64) {
+    auto count = [&](int b) {
         const int from = a.t.tok_start[b], to = a.t.tok_start[b + 1];
         const Seq s = make_seq(from, to, a.t.seq_len[b], a.t.n_tokens, int64_t(a.t.max_pages) << a.t.page_shift, a.window,
                                a.group_shift);
-        if (b < 64) p.mine = s;
         wrong |= from != s.start || to != s.start + s.nq;
         W += uint64_t(s.tiles) * uint64_t(s.len);
         T += s.tiles;
         mx = mx > s.len ? mx : s.len;
-    }
+        return s;
+    };
+    const bool many = a.t.B > 64;
+    if (!many && lane < a.t.B) p.mine = count(lane);
     p.chunk = 1 << 30;
     if (a.splits == 1) return p;
-    p.chunk = 0;
-    if (__any(wrong)) return p;
+    if (many) {
+        const int per = (a.t.B + 255) / 256, b0 = threadIdx.x * per, b1 = b0 + per < a.t.B ? b0 + per : a.t.B;
+#pragma unroll 4
+        for (int b = b0; b < b1; ++b) count(b);
+    }
     if (a.t.B > 1) {
 #pragma unroll
         for (int k = 1; k < 64; k *= 2) {
@@ -108,6 +116,25 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, int lane) {
             mx = mx > y ? mx : y;
         }
     }
+    wrong = __any(wrong);
+    if (many) {
+        struct Part { uint64_t W; int T, mx, wrong, pad; };
+        Part *part = reinterpret_cast<Part *>(lds);
+        if (lane == 0) part[threadIdx.x >> 6] = Part{W, T, mx, wrong, 0};
+        __syncthreads();
+        W = 0;
+        T = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            W += part[w].W;
+            T += part[w].T;
+            mx = mx > part[w].mx ? mx : part[w].mx;
+            wrong |= part[w].wrong != 0;
+        }
+        __syncthreads();
+    }
+    p.chunk = 0;
+    if (wrong) return p;
     W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
     p.tiles = __builtin_amdgcn_readfirstlane(T);
     p.longest = __builtin_amdgcn_readfirstlane(mx);
@@ -116,39 +143,70 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, int lane) {
 }
 
 // Pair x of the call: sequences in order, chunks of a sequence in order, tiles last first (the later
-// tokens of a chunk see more keys).  kTiles: tile x instead, as its first chunk's item.
+// tokens of a chunk see more keys).  kTiles: tile x instead, as its first chunk's item.  x and so the result are
+// the same in all threads.  lds as above.
 template <bool kTiles = false>
-__device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, const Plan &p, int *b_out, int *c_out, Item *it) {
+__device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, const Plan &p, unsigned char *lds, int *b_out,
+                                 int *c_out, Item *it) {
     const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
-    uint32_t before = 0;
-    for (int b0 = 0; b0 < a.t.B; b0 += 64) {
-        uint32_t n = 0;
-        Seq s = p.mine;
-        if (b0 + lane < a.t.B) {
-            if (b0 > 0) s = load_seq(a, b0 + lane);
-            n = uint32_t(s.tiles) * uint32_t(kTiles ? 1 : chunks_of(s, p.chunk));
-        }
-        uint32_t incl = n;
-        if (a.t.B > 1) {
+    auto pairs = [&](const Seq &s) { return uint32_t(s.tiles) * uint32_t(kTiles ? 1 : chunks_of(s, p.chunk)); };
+    const bool many = a.t.B > 64;
+    const int per = (a.t.B + 255) / 256, b0 = threadIdx.x * per, b1 = b0 + per < a.t.B ? b0 + per : a.t.B;
+    uint32_t n = 0;
+    if (many) {
+#pragma unroll 4
+        for (int b = b0; b < b1; ++b) n += pairs(load_seq(a, b));
+    } else if (lane < a.t.B) {
+        n = pairs(p.mine);
+    }
+    uint32_t incl = n;
+    if (a.t.B > 1) {
 #pragma unroll
-            for (int k = 1; k < 64; k *= 2) {
-                const uint32_t y = __shfl_up(incl, k);
-                incl += lane >= k ? y : 0u;
+        for (int k = 1; k < 64; k *= 2) {
+            const uint32_t y = __shfl_up(incl, k);
+            incl += lane >= k ? y : 0u;
+        }
+    }
+    Seq s;
+    uint32_t in;
+    if (many) {
+        uint32_t *total = reinterpret_cast<uint32_t *>(lds), *found = total + 4;
+        if (lane == 63) total[threadIdx.x >> 6] = incl;
+        if (threadIdx.x == 0) found[0] = ~0u;
+        __syncthreads();
+        uint32_t from = incl - n;
+#pragma unroll
+        for (int w = 0; w < 3; ++w) from += w < int(threadIdx.x >> 6) ? total[w] : 0u;
+        if (x >= from && x - from < n) {                     // one thread at most
+            in = x - from;
+            for (int b = b0; b < b1; ++b) {
+                const uint32_t k = pairs(load_seq(a, b));
+                if (in < k) {
+                    found[0] = uint32_t(b);
+                    found[1] = in;
+                    break;
+                }
+                in -= k;
             }
         }
-        const unsigned long long past = __ballot(before + incl > x);
-        if (past) {
-            const int l = __ffsll(past) - 1;
-            const uint32_t in = x - before - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l));
-            s = of_lane(s, l);
-            *b_out = b0 + l;
-            *c_out = int(in / uint32_t(s.tiles));
-            *it = make_item(s, s.tiles - 1 - int(in % uint32_t(s.tiles)), *c_out, p.chunk, cap, a.window, a.group_shift);
-            return !it->idle;
-        }
-        before += __builtin_amdgcn_readlane(incl, 63);
+        __syncthreads();
+        const int b = __builtin_amdgcn_readfirstlane(found[0]);
+        in = __builtin_amdgcn_readfirstlane(found[1]);
+        __syncthreads();
+        if (b < 0) return false;
+        *b_out = b;
+        s = of_lane(load_seq(a, b), 0);
+    } else {
+        const unsigned long long past = __ballot(incl > x);
+        if (!past) return false;
+        const int l = __ffsll(past) - 1;
+        in = x - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l));
+        s = of_lane(p.mine, l);
+        *b_out = l;
     }
-    return false;
+    *c_out = int(in / uint32_t(s.tiles));
+    *it = make_item(s, s.tiles - 1 - int(in % uint32_t(s.tiles)), *c_out, p.chunk, cap, a.window, a.group_shift);
+    return !it->idle;
 }
 
 // Pool row of the 16 keys at `pos` of sequence b and head g; -1 behind `end` or on a page outside the

@@ -243,7 +243,7 @@ def test_offsets_past_2_31(S):
     assert ws.status() == 0
 
 
-@pytest.mark.parametrize("batch", [1, 64, 65, 200])
+@pytest.mark.parametrize("batch", [1, 64, 65, 200, 257, 1100])
 def test_many_sequences(S, batch):
     """More sequences than lanes: the same results as each sequence by itself."""
     rng = np.random.default_rng(batch)
