@@ -55,9 +55,9 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
             for (int e = 0; e < VE; ++e) so[(wave * N + 16 * nb + n) * RS + VE * (4 * gq + i) + e] = r.o[nb][e][i];
     }
     if (__syncthreads_or(bad)) return true;
-    const int d0 = (threadIdx.x & 15) * VE;
+    const int d0 = (threadIdx.x & 15) * 2;                   // and 32, 64, .. on: what 16 threads store lies together
     for (int rw = threadIdx.x >> 4; rw < it.rows; rw += 16) {
-        float m = -INFINITY, sum = 0.f, o[VE] = {};
+        float m = -INFINITY, sum = 0.f, o[VE / 2][2] = {};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w * 2 * N + rw]);
         const float mu = m == -INFINITY ? 0.f : m;
@@ -66,9 +66,16 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
             const float f = exp2_fast(ml[w * 2 * N + rw] - mu);
             sum += f * ml[w * 2 * N + N + rw];
 #pragma unroll
-            for (int e = 0; e < VE; ++e) o[e] += f * so[(w * N + rw) * RS + d0 + e];
+            for (int e = 0; e < VE / 2; ++e) {
+                const float *p = so + (w * N + rw) * RS + d0 + 32 * e;
+                o[e][0] += f * p[0];
+                o[e][1] += f * p[1];
+            }
         }
-        put<T, D>(a, it, c, it.tok0 + (rw >> a.group_shift), (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1)), d0, o, m, sum);
+#pragma unroll
+        for (int e = 0; e < VE / 2; ++e)
+            put<T, D>(a, it, c, it.tok0 + (rw >> a.group_shift), (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1)),
+                      d0 + 32 * e, o[e], m, sum);
     }
     return false;
 }
