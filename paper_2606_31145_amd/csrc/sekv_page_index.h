@@ -14,7 +14,11 @@
 // the lengths are alike, k full rounds of items cost k (L / n + over) with n = k slots / T chunks a
 // tile; the best of a few k is taken, or no cut at all.  Where they differ, the time is at most
 // (W + (W / chunk) over) / slots + chunk, the last term being the item that ends last; that is least
-// at chunk = sqrt(W over / slots).  Measured (us): `over` of 64, 128 and 256 keys where partials are joined
+// at chunk = sqrt(W over / slots).  Where a tile's last workgroup joins its partials, each chunk costs it about one
+// key's time a row as well: a longest sequence of L keys then asks for no more than sqrt(L / rows) chunks.
+// With and without that term: nine tokens of 2 heads over 35714 keys of one KV head 40 and 112 us, two of 4 over
+// 14199 of two 16 and 32, four of 11 ragged sequences of up to 22057 30 and 42, one over 2048 10.4 and 12.5.
+// Measured (us): `over` of 64, 128 and 256 keys where partials are joined
 // in the last workgroup: one token of 8 users at 9000 in 8 bits 34.6, 34.7, 34.7; of 256, 512 and 1024 where
 // a second kernel joins them: 13 ragged sequences, one of 257 tokens, 97.3, 96.4, 90.9, one of 257 alone 65.0,
 // 65.0, 64.6.  Steps of 64 and 128 keys: 333 float tokens at 3000 86.4 and 94.5, one token at 2048 9.9 and 10.6.
@@ -40,7 +44,12 @@ constexpr int kFewRows = 64;       // rows of two narrow tiles, which read the k
 constexpr int kTileRows = 128;     // 32 rows for each of four waves
 constexpr int kChunkStep = 64;     // keys: a tile of the wide form, one or two steps of four waves in the narrow one
 constexpr int kSlots = 512;        // workgroups that run at once: two on each of 256 compute units
-constexpr int kOverNarrow = 128, kOverWide = 1024;    // keys that an item costs beside its own
+constexpr int kOver = 128, kOverWide = 1024;     // keys that an item costs beside its own; of the wide bfloat16 form
+SEKV_HD int over_of(bool wide, bool is_float) { return wide && !is_float ? kOverWide : kOver; }
+// What the join of a chunk costs the last workgroup of a tile, in keys; a second kernel spreads it.
+SEKV_HD float join_rows_of(bool wide, int n_tokens, int group_shift, int T) {
+    return wide || T < 1 ? 0.f : float(int64_t(n_tokens) << group_shift) / float(T);
+}
 constexpr int kBlock = 16;         // keys that lie in one page: the smallest page
 
 // Pool row of position `pos` (below max_pages * page_size) from its table entry; -1 when the page is
@@ -81,24 +90,28 @@ SEKV_HD Seq make_seq(int start, int end, int seq_len, int n_tokens, int64_t cap,
 SEKV_HD uint64_t quotient(uint64_t a, uint32_t b) { return a >> 32 ? a / b : uint64_t(uint32_t(a) / b); }
 
 // W, T: of one KV head
-SEKV_HD int chunk_length(uint64_t W, int T, int max_len, int Hkv, int target, int splits, int over) {
+SEKV_HD int chunk_length(uint64_t W, int T, int max_len, int Hkv, int target, int splits, int over, float rows) {
     if (T < 1) return kChunkStep;
     uint64_t c = quotient(W + target - 1, uint32_t(target));
     const uint32_t d = (uint32_t(max_len) + uint32_t(splits) - 1) / uint32_t(splits);
     c = c > d ? c : d;
-    const float mean = float(W) / float(T), all = float(T) * float(Hkv);
+    const float mean = float(W) / float(T), all = float(T) * float(Hkv), len = float(max_len);
     float best = float(max_len);                             // no cut
     if (float(max_len) <= 1.1f * mean) {
         const int rounds = int((all + float(kSlots - 1)) / float(kSlots));
         float cost = float(rounds) * float(max_len);
-        for (int k = 1; k <= 4; ++k) {
-            const float n = float(int(float(k * kSlots) / all));
-            const float x = n > 1.f ? float(k) * (float(max_len) / n + float(over)) : cost;
-            best = x < cost ? float(max_len) / n : best;
+        for (int k = 0; k <= 4; ++k) {
+            float n = float(int(float((k ? k : 1) * kSlots) / all));
+            if (k == 0) {                                    // fewer chunks than fill the device
+                const float few = sqrtf(len / (rows + 1e-3f));
+                n = n < few ? n : few;
+            }
+            const float x = n > 1.f ? float(k ? k : 1) * (len / n + float(over)) + n * rows : cost;
+            best = x < cost ? len / n : best;
             cost = x < cost ? x : cost;
         }
     } else {
-        const float x = sqrtf(mean * all * float(over) / float(kSlots));
+        const float x = sqrtf(mean * all * float(over) / float(kSlots) + len * rows);
         best = x < best ? x : best;
     }
     const uint32_t m = uint32_t(best) + 1;

@@ -83,7 +83,7 @@ struct Plan {
 };
 
 // lds: 256 bytes, free again on return.
-__device__ inline Plan make_plan(const PageAttendArgs &a, int lane, unsigned char *lds) {
+__device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, int lane, unsigned char *lds) {
     Plan p;
     uint64_t W = 0;
     int mx = 0, T = 0;
@@ -138,7 +138,8 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, int lane, unsigned cha
     W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
     p.tiles = __builtin_amdgcn_readfirstlane(T);
     p.longest = __builtin_amdgcn_readfirstlane(mx);
-    p.chunk = chunk_length(W, p.tiles, p.longest, a.t.Hkv, a.target, a.splits, a.join_launch ? kOverWide : kOverNarrow);
+    p.chunk = chunk_length(W, p.tiles, p.longest, a.t.Hkv, a.target, a.splits, over_of(a.join_launch, is_float),
+                           join_rows_of(a.join_launch, a.t.n_tokens, a.group_shift, p.tiles));
     return p;
 }
 

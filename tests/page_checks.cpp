@@ -50,7 +50,8 @@ static void walk(const Tables &t, int Hkv, int gs, int64_t cap, int window, int 
         T += s.tiles;
         mx = mx > s.len ? mx : s.len;
     }
-    const int chunk = l.splits == 1 ? 1 << 30 : chunk_length(W, T, mx, Hkv, l.target, l.splits, join_in_launch(B, t.n_tokens, gs) ? kOverWide : kOverNarrow);
+    const int chunk = l.splits == 1 ? 1 << 30 : chunk_length(W, T, mx, Hkv, l.target, l.splits, over_of(join_in_launch(B, t.n_tokens, gs), Hkv % 2 != 0),
+                                                                  join_rows_of(join_in_launch(B, t.n_tokens, gs), t.n_tokens, gs, T));
     REQUIRE(chunk % kChunkStep == 0);
     std::vector<std::vector<int>> seen(t.n_tokens);
     for (auto &v : seen) v.assign(size_t(cap), 0);
