@@ -134,12 +134,14 @@ struct Item {
 
 SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, int window, int group_shift) {
     Item it;
-    it.narrow = (s.nq << group_shift) <= kFewRows;
-    const int per = (it.narrow ? kNarrowRows : kTileRows) >> group_shift;
+    const int per = ((s.nq << group_shift) <= kFewRows ? kNarrowRows : kTileRows) >> group_shift;
     const int t0 = tile * per, left = s.nq - t0;
     it.tok0 = s.start + t0;
     it.n_tok = left < per ? left : per;
     it.rows = it.n_tok << group_shift;
+    // The rest behind tiles of 128 rows is narrow, too: 13 ragged sequences, one of 257 tokens, 687 us against 739
+    // in float, 89.3 against 90.6 in bfloat16.
+    it.narrow = it.rows <= kNarrowRows;
     it.p0 = s.first + t0;
     const int64_t b64 = it.p0 - (int64_t(window) - 1), e64 = it.p0 + it.n_tok;
     const uint32_t b = b64 < 0 ? 0u : b64 < cap ? uint32_t(b64) & ~63u : uint32_t(cap);
