@@ -154,6 +154,9 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     auto partial = [&](int pos, uint32_t valid) { return valid != 15u || pos < all_lo || pos + 63 > all_hi; };
     const lds_bytes tile = (lds_bytes)lds;
     const int own = wave * 16;
+    // rows of a tile that hold keys which some row of the item sees
+    const int first = int(it.p0 - (int64_t(a.window) - 1) > 0 ? it.p0 - (int64_t(a.window) - 1) : 0);   // below it.end
+    auto from_of = [&](int pos) { return first - pos; };
     auto end_of = [&](int pos, uint32_t valid) { return valid >> wave & 1 ? it.end - pos : 0; };
     int pos = it.begin, mine = -1;
     uint32_t valid = rows_of(pos, page_of(pos), &mine), ahead = 0;
@@ -163,7 +166,7 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
         dr.load(a, mine, tile, tile + 2 * kTile, own);
     } else {
         st.load(a, mine, lane);
-        if (partial(pos, valid)) bad |= st.mend(own, end_of(pos, valid), lane);
+        if (partial(pos, valid)) bad |= st.mend(own, from_of(pos), end_of(pos, valid), lane);
         st.store(lds, lds + 2 * kTile, own, lane);
     }
     arrived();
@@ -172,7 +175,7 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
         constexpr int B = decltype(kBuf)::value;
         const bool more = pos + 64 < it.end;
         if (kDirect && partial(pos, valid)) {
-            bad |= dr.mend(lds + (2 + B) * kTile, own, end_of(pos, valid), lane);
+            bad |= dr.mend(lds + (2 + B) * kTile, own, from_of(pos), end_of(pos, valid), lane);
             __syncthreads();
         }
         const bool part = partial(pos, valid), rows = wave * 32 < it.rows;
@@ -187,7 +190,7 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
             if (more) st.load(a, mine, lane);
             if (rows) r.step(a, tile + B * kTile, tile + (2 + B) * kTile, pos, valid, part, lane);
             if (more) {
-                if (partial(pos + 64, ahead)) bad |= st.mend(own, end_of(pos + 64, ahead), lane);
+                if (partial(pos + 64, ahead)) bad |= st.mend(own, from_of(pos + 64), end_of(pos + 64, ahead), lane);
                 st.store(lds + (1 - B) * kTile, lds + (3 - B) * kTile, own, lane);
             }
         }

@@ -513,6 +513,8 @@ struct Rows16 {
                     const int key = pos + 16 * j + 4 * g + i;
                     const uint32_t keep = (valid >> j & 1) && key >= lo_any && key <= hi_any ? 0xffffffffu : 0u;
                     uint32_t wrong = 0;
+                    // the exponent byte as well: one of 255 makes no number of any code
+                    if constexpr (P::kBytes == 1) t.vs[j] = keep ? t.vs[j] : (t.vs[j] & ~(255u << (8 * i))) | 127u << (8 * i);
 #pragma unroll
                     for (int w = 0; w < Tile::VW; ++w) {
                         t.v[j][i][w] &= keep;

@@ -70,13 +70,15 @@ struct Stage {
             vs[i] = a.v_scale[r0 + i * (64 / PC) + lane / PC];
         }
     }
-    // For a tile that not every row sees: values from row `end` on, which none sees, become zeros.  True when
-    // another holds a NaN: the product with its masked weight, zero, would be no number.
-    __device__ bool mend(int row0, int end, int lane) {
+    // For a tile that not every row sees: values before row `from` and from row `end` on, which none sees, become
+    // zeros, their exponent bytes those of one (255 makes no number of any code).  True when another holds a NaN:
+    // the product with its masked weight, zero, would be no number.
+    __device__ bool mend(int row0, int from, int end, int lane) {
         uint32_t bad = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint32_t keep = row0 + i * (64 / PC) + lane / PC >= end ? 0u : ~0u;
+            const int row = row0 + i * (64 / PC) + lane / PC;
+            const uint32_t keep = row >= from && row < end ? ~0u : 0u;
             v[i] &= keep;
             vs[i] = keep ? vs[i] : 127u;
             bad |= nan4(v[i].x) | nan4(v[i].y) | nan4(v[i].z) | nan4(v[i].w);
@@ -127,12 +129,13 @@ struct Direct {
         }
     }
     // as Stage::mend, infinities too, for the tile's rows row .. row + 15
-    __device__ bool mend(unsigned char *vt, int row, int end, int lane) const {
+    __device__ bool mend(unsigned char *vt, int row, int from, int end, int lane) const {
         uint32_t bad = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             uint4 *p = reinterpret_cast<uint4 *>(vt + row * (D * 2) + i * 1024 + lane * 16);
-            const uint32_t keep = row + i * (64 / PC) + lane / PC >= end ? 0u : ~0u;
+            const int at = row + i * (64 / PC) + lane / PC;
+            const uint32_t keep = at >= from && at < end ? ~0u : 0u;
             uint4 w = *p;
             w = make_uint4(w.x & keep, w.y & keep, w.z & keep, w.w & keep);
             *p = w;
