@@ -47,6 +47,8 @@ __device__ inline float across16(float x) {
 __device__ inline uint32_t odd2(uint32_t w) { return uint32_t((w & 0x7f80u) == 0x7f80u) | uint32_t((w & 0x7f800000u) == 0x7f800000u); }
 __device__ inline uint32_t odd(const uint4 &v) { return odd2(v.x) | odd2(v.y) | odd2(v.z) | odd2(v.w); }
 __device__ inline bool odd(float x) { return !(fabsf(x) <= 3.402823466e38f); }
+// The first exponent byte whose rows may decode to infinities: 256 * 2^120 is past float and bfloat16.
+constexpr uint32_t kOverExponent = 247;
 // Is one of four e4m3 codes a NaN.
 __device__ inline uint32_t nan4(uint32_t w) {
     const uint32_t x = ~w & 0x7f7f7f7fu;               // a zero byte: NaN
@@ -502,7 +504,8 @@ struct Rows16 {
     }
 
     // o += values x weights.  Where `part`, rows that no column sees count as zeros, and `bad` says that one
-    // which some columns do not see holds an infinity or NaN: zero times that is no number.
+    // which some columns do not see holds an infinity or NaN, or 8-bit values that may become one: zero times
+    // that is no number.
     __device__ void values(Tile &t, const f4v (&s)[J][NB], int pos, uint32_t valid, bool part, bool *bad, int lane) {
         const int g = lane >> 4;
         if (part) {
@@ -514,7 +517,10 @@ struct Rows16 {
                     const uint32_t keep = (valid >> j & 1) && key >= lo_any && key <= hi_any ? 0xffffffffu : 0u;
                     uint32_t wrong = 0;
                     // the exponent byte as well: one of 255 makes no number of any code
-                    if constexpr (P::kBytes == 1) t.vs[j] = keep ? t.vs[j] : (t.vs[j] & ~(255u << (8 * i))) | 127u << (8 * i);
+                    if constexpr (P::kBytes == 1) {
+                        t.vs[j] = keep ? t.vs[j] : (t.vs[j] & ~(255u << (8 * i))) | 127u << (8 * i);
+                        wrong = uint32_t((t.vs[j] >> (8 * i) & 255u) >= kOverExponent);
+                    }
 #pragma unroll
                     for (int w = 0; w < Tile::VW; ++w) {
                         t.v[j][i][w] &= keep;

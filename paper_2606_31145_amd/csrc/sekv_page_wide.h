@@ -71,8 +71,8 @@ struct Stage {
         }
     }
     // For a tile that not every row sees: values before row `from` and from row `end` on, which none sees, become
-    // zeros, their exponent bytes those of one (255 makes no number of any code).  True when another holds a NaN:
-    // the product with its masked weight, zero, would be no number.
+    // zeros, their exponent bytes those of one (255 makes no number of any code).  True when another holds a NaN,
+    // or values that may decode to infinity: the product with its masked weight, zero, would be no number.
     __device__ bool mend(int row0, int from, int end, int lane) {
         uint32_t bad = 0;
 #pragma unroll
@@ -81,7 +81,7 @@ struct Stage {
             const uint32_t keep = row >= from && row < end ? ~0u : 0u;
             v[i] &= keep;
             vs[i] = keep ? vs[i] : 127u;
-            bad |= nan4(v[i].x) | nan4(v[i].y) | nan4(v[i].z) | nan4(v[i].w);
+            bad |= uint32_t(vs[i] >= kOverExponent) | nan4(v[i].x) | nan4(v[i].y) | nan4(v[i].z) | nan4(v[i].w);
         }
         return bad != 0;
     }
@@ -128,7 +128,7 @@ struct Direct {
             __builtin_amdgcn_global_load_lds((global)(vp + voff[i]), vt + row * (D * 2) + i * 1024, 16, 0, 0);
         }
     }
-    // as Stage::mend, infinities too, for the tile's rows row .. row + 15
+    // as Stage::mend, for the tile's rows row .. row + 15
     __device__ bool mend(unsigned char *vt, int row, int from, int end, int lane) const {
         uint32_t bad = 0;
 #pragma unroll
