@@ -355,7 +355,8 @@ SEKV_API sekv_status sekv_build_cache(const sekv_build_dims *dims, const void *k
  * Bad tables give a wrong answer and error bit 8, never an access outside the buffers: a page
  * outside [0, n_pages) takes no part (not written, not read, its keys not seen), nor does a
  * token at a position below 0 (for sekv_page_append) or at max_pages * page_size and behind.
- * Entries of the table behind a sequence's last token are not read.  Two rows of one
+ * Entries of the table behind a sequence's last token are not read, nor by sekv_page_attend those of
+ * pages before the first key that one of the sequence's new tokens sees.  Two rows of one
  * sekv_page_append that fall into the same slot race: share pages between sequences only
  * where none of their rows is written.
  * -------------------------------------------------------------------------------- */

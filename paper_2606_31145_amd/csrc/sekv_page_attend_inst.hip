@@ -143,11 +143,11 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     // them hold keys
     auto page_of = [&](int pos) {
         const int p = pos + 16 * (lane & 3);
-        return p < it.end ? a.t.table[int64_t(b) * a.t.max_pages + (p >> a.t.page_shift)] : -1;
+        return block_seen(it, p) ? a.t.table[int64_t(b) * a.t.max_pages + (p >> a.t.page_shift)] : -1;
     };
     auto rows_of = [&](int pos, int page, int *mine) {
         const int p = pos + 16 * (lane & 3), row = block_row(page, a.t.n_pages, a.t.Hkv, g, a.t.page_shift, p);
-        if (row < 0 && p < it.end && lane < 4) flag(a.t);
+        if (row < 0 && block_seen(it, p) && lane < 4) flag(a.t);
         *mine = __builtin_amdgcn_readlane(row, wave);
         return uint32_t(__ballot(row >= 0)) & 15u;
     };
@@ -155,8 +155,7 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     const lds_bytes tile = (lds_bytes)lds;
     const int own = wave * 16;
     // rows of a tile that hold keys which some row of the item sees
-    const int first = int(it.p0 - (int64_t(a.window) - 1) > 0 ? it.p0 - (int64_t(a.window) - 1) : 0);   // below it.end
-    auto from_of = [&](int pos) { return first - pos; };
+    auto from_of = [&](int pos) { return it.first - pos; };
     auto end_of = [&](int pos, uint32_t valid) { return valid >> wave & 1 ? it.end - pos : 0; };
     int pos = it.begin, mine = -1;
     uint32_t valid = rows_of(pos, page_of(pos), &mine), ahead = 0;

@@ -127,6 +127,7 @@ struct Item {
     int rows;             // n_tok << group_shift
     bool narrow;
     int64_t p0;           // position of its first token
+    int first;            // first key that one of its rows sees (at most the capacity)
     int begin, end;       // keys (begin a multiple of 64); empty when begin >= end
     int chunk0, chunk1;   // first and last chunk with keys of the tile; equal: no join is needed
     bool idle;            // nothing to do
@@ -146,6 +147,7 @@ SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, in
     const int64_t b64 = it.p0 - (int64_t(window) - 1), e64 = it.p0 + it.n_tok;
     const uint32_t b = b64 < 0 ? 0u : b64 < cap ? uint32_t(b64) & ~63u : uint32_t(cap);
     const uint32_t e = e64 < 0 ? 0u : e64 < cap ? uint32_t(e64) : uint32_t(cap);
+    it.first = int(b64 < 0 ? 0 : b64 < cap ? b64 : cap);
     it.begin = it.end = 0;
     it.chunk0 = it.chunk1 = 0;
     it.idle = c != 0;
@@ -159,6 +161,10 @@ SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, in
     it.end = int(e < ce ? e : ce);
     return it;
 }
+
+// Whether some row of the item sees a key of the block at pos.  An item begins at a multiple of 64, so under a
+// window its first blocks may lie before every row's: their page may be somebody else's by then, or none.
+SEKV_HD bool block_seen(const Item &it, int pos) { return pos < it.end && pos + kBlock > it.first; }
 
 // Host side: grid and workspace of a call.
 struct Launch {

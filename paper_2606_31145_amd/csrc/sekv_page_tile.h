@@ -212,10 +212,10 @@ __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, 
     return !it->idle;
 }
 
-// Pool row of the 16 keys at `pos` of sequence b and head g; -1 behind `end` or on a page outside the
-// pool.  Uniform in the wave: read through the scalar cache.
-__device__ inline int key_block(const PageAttendArgs &a, int b, int g, int pos, int end, int lane) {
-    if (pos >= end) return -1;
+// Pool row of the 16 keys at `pos` of sequence b and head g; -1 where the item sees none of them or on a page
+// outside the pool.  Uniform in the wave: read through the scalar cache.
+__device__ inline int key_block(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int lane) {
+    if (!block_seen(it, pos)) return -1;
     typedef const __attribute__((address_space(4))) int32_t *ro;
     const int page = ((ro)(uintptr_t)a.t.table)[int64_t(b) * a.t.max_pages + (pos >> a.t.page_shift)];
     const int r = block_row(page, a.t.n_pages, a.t.Hkv, g, a.t.page_shift, pos);
@@ -628,7 +628,7 @@ struct Rows16 {
     }
     __device__ static void look(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int (&row)[J], int lane) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) row[j] = key_block(a, b, g, pos + 16 * j, it.end, lane);
+        for (int j = 0; j < J; ++j) row[j] = key_block(a, it, b, g, pos + 16 * j, lane);
     }
 
     // The column's sum over its four lanes.
