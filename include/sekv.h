@@ -346,10 +346,10 @@ SEKV_API sekv_status sekv_build_cache(const sekv_build_dims *dims, const void *k
  * and subnormal ones).  Infinities and NaN are stored as NaN in 8 bits.
  *
  * Ragged batches: the new tokens of all sequences lie one after another; sequence b has rows
- * tok_start[b] .. tok_start[b + 1] - 1 of n_tokens (tok_start int32 [B + 1], ascending from 0;
- * rows at tok_start[B] and behind belong to nobody and no output row of theirs is written).  seq_len[b] counts the
- * sequence's tokens with the new ones, so new token i of n_new stands at position
- * seq_len[b] - n_new + i.  Both tables are read on the device: a captured graph may be
+ * tok_start[b] .. tok_start[b + 1] - 1 of n_tokens (tok_start int32 [B + 1], never descending, within 0 and
+ * n_tokens; rows before tok_start[0], at tok_start[B] and behind belong to nobody and no output row of theirs
+ * is written).  seq_len[b] counts the sequence's tokens with the new ones, so new token i of n_new stands at
+ * position seq_len[b] - n_new + i.  Both tables are read on the device: a captured graph may be
  * replayed with other contents.
  *
  * Bad tables give a wrong answer and error bit 8, never an access outside the buffers: a page

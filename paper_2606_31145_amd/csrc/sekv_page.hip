@@ -92,7 +92,7 @@ template <> struct Piece<BF16> {
 
 // The place of new token `tok`: its sequence by a search in `start` (LDS), its row in the pool, or -1 (flagged).
 __device__ inline int place(const PageTables &t, const int32_t *start, int tok, int g, bool first_lane) {
-    if (tok >= start[t.B] || tok < start[0]) return -1;      // behind the last sequence
+    if (tok >= start[t.B] || tok < start[0]) return -1;      // nobody's
     int lo = 0, hi = t.B;                                    // the last b with start[b] <= tok
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -180,6 +180,11 @@ __global__ void __launch_bounds__(kThreads) append_kernel(PageAppendArgs a) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) store_row<T, P, D>(a, s, to, w[s], lane);
         }
+    }
+    if (blockIdx.x == 0) {                                   // offsets that cannot be
+        bool wrong = start[0] < 0 || start[t.B] > t.n_tokens;
+        for (int i = threadIdx.x; i < t.B; i += kThreads) wrong |= start[i] > start[i + 1];
+        if (wrong) flag(t);
     }
 }
 
