@@ -223,6 +223,7 @@ __global__ void __launch_bounds__(kThreads) read_kernel(PageReadArgs a) {
         const int64_t bg = c / chunks;
         const int b = int(bg / t.Hkv), g = int(bg % t.Hkv), pos = int(c % chunks) * 64 + wave * 16;
         const int have = t.seq_len[b] < a.max_tokens ? t.seq_len[b] : a.max_tokens;
+        if (have < 0 && pos == 0 && lane == 0) flag(t);      // a length that cannot be
         if (pos >= have) continue;
         const int from = (pos >> t.page_shift) < t.max_pages ? pool_row(t, b, g, pos) : -1;
         if (from < 0) {

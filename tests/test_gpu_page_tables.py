@@ -53,3 +53,14 @@ def test_offsets_may_leave_rows_out_on_both_sides(S):
     want, _ = S.page_attend(c.dims(S), other, c.q.cuda(), c.tok_start(), ws)
     assert torch.equal(out[2:-1], want) and (out[:2] == -3.0).all() and (out[-1:] == -3.0).all()
     assert ws.status() == 0
+
+
+@pytest.mark.parametrize("store", ["same", "e4m3"])
+def test_read_flags_a_negative_length(S, store):
+    c = Case("bf16", store, [40, 20], [0, 0], dim=64, page=16)
+    cache, ws = c.cache(S), c.workspace(S)
+    want, _ = S.page_read(c.dims(S), cache, 48, ws)
+    assert ws.status() == 0
+    cache.seq_len[0] = -1
+    keys, _ = S.page_read(c.dims(S), cache, 48, ws)
+    assert ws.status() == 8 and not keys[0].any() and torch.equal(keys[1], want[1])
