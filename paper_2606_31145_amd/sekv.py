@@ -819,6 +819,13 @@ def _on(device, stream):
     return torch.cuda.stream(stream), stream.cuda_stream
 
 
+def _page_ws(ws: Workspace, device):
+    """(address, bytes) of a call's workspace, which the kernels write to: on the pages' device."""
+    if ws.tensor.device != device:
+        raise ValueError(f"the workspace is on {ws.tensor.device}, the pages on {device}")
+    return ws.ptr, ws.nbytes
+
+
 def page_append(pd: PageDims, cache: PageCache, k, v, tok_start, ws: Workspace, stream=None):
     """sekv_page_append: stores k, v [n_tokens][Hkv][d] (tokens may be strided) in the pages."""
     cs, dev = cache.struct(pd), cache.k_pages.device
@@ -829,7 +836,7 @@ def page_append(pd: PageDims, cache: PageCache, k, v, tok_start, ws: Workspace, 
     ts = _tok_start(pd, tok_start, dev)
     ctx, st = _on(dev, stream)
     with ctx:
-        _check(LIB.sekv_page_append(pd, cs, kp, vp, sk, sv, ts, len(k), ws.ptr, ws.nbytes, st))
+        _check(LIB.sekv_page_append(pd, cs, kp, vp, sk, sv, ts, len(k), *_page_ws(ws, dev), st))
 
 
 def page_read(pd: PageDims, cache: PageCache, max_tokens: int, ws: Workspace, keys=None, values=None, stream=None):
@@ -845,7 +852,7 @@ def page_read(pd: PageDims, cache: PageCache, max_tokens: int, ws: Workspace, ke
             values = torch.zeros(shape, dtype=dt, device=dev)
         _expect(keys, "keys", dt, shape, dev)
         _expect(values, "values", dt, shape, dev)
-        _check(LIB.sekv_page_read(pd, cs, _ptr(keys), _ptr(values), int(max_tokens), ws.ptr, ws.nbytes, st))
+        _check(LIB.sekv_page_read(pd, cs, _ptr(keys), _ptr(values), int(max_tokens), *_page_ws(ws, dev), st))
     return keys, values
 
 
@@ -866,7 +873,7 @@ def page_attend(pd: PageDims, cache: PageCache, q, tok_start, ws: Workspace, out
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
         elif lse is not None:
             _expect(lse, "lse", torch.float32, q.shape[:2], dev)
-        _check(LIB.sekv_page_attend(pd, cs, qp, sq, ts, len(q), _ptr(out), _ptr(lse), ws.ptr, ws.nbytes, st))
+        _check(LIB.sekv_page_attend(pd, cs, qp, sq, ts, len(q), _ptr(out), _ptr(lse), *_page_ws(ws, dev), st))
     return out, lse
 
 
