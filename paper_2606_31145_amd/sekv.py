@@ -882,5 +882,7 @@ def build_layer_paged(bd: BuildDims, pd: PageDims, cache: PageCache, surprisal, 
     read back and become the layer's span cache."""
     if (bd.batch, bd.n_kv_heads, bd.head_dim, bd.dtype) != (pd.batch, pd.n_kv_heads, pd.head_dim, pd.dtype):
         raise ValueError("build and page dims differ in batch, KV heads, head_dim or dtype")
-    keys, values = page_read(pd, cache, bd.max_tokens, ws, stream=stream)
-    return build_layer(bd, keys, values, surprisal, cache.seq_len, omega, ws, stream)
+    ctx, _ = _on(cache.k_pages.device, stream)
+    with ctx:                                                # what the builder allocates and clears, too
+        keys, values = page_read(pd, cache, bd.max_tokens, ws)
+        return build_layer(bd, keys, values, surprisal, cache.seq_len, omega, ws)
