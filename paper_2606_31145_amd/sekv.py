@@ -878,11 +878,15 @@ def page_attend(pd: PageDims, cache: PageCache, q, tok_start, ws: Workspace, out
 
 
 def build_layer_paged(bd: BuildDims, pd: PageDims, cache: PageCache, surprisal, omega, ws: Workspace, stream=None):
-    """build_layer on the rows of a paged store: every sequence's stored tokens (cache.seq_len) are
-    read back and become the layer's span cache."""
+    """build_layer on the rows of a paged store: every sequence's stored tokens (cache.seq_len, at most
+    bd.max_tokens) are read back and become the layer's span cache."""
     if (bd.batch, bd.n_kv_heads, bd.head_dim, bd.dtype) != (pd.batch, pd.n_kv_heads, pd.head_dim, pd.dtype):
         raise ValueError("build and page dims differ in batch, KV heads, head_dim or dtype")
+    cache.struct(pd)
     ctx, _ = _on(cache.k_pages.device, stream)
     with ctx:                                                # what the builder allocates and clears, too
+        for b, n in enumerate(cache.seq_len.tolist()):
+            if not 0 <= n <= bd.max_tokens:
+                raise ValueError(f"sequence {b} has {n} tokens, the build dims' max_tokens is {bd.max_tokens}")
         keys, values = page_read(pd, cache, bd.max_tokens, ws)
         return build_layer(bd, keys, values, surprisal, cache.seq_len, omega, ws)

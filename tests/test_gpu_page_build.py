@@ -1,4 +1,5 @@
-"""build_layer_paged on another stream, given as an object or as a handle, with the default stream busy."""
+"""build_layer_paged on another stream, given as an object or as a handle, with the default stream busy;
+and lengths that the builder's dims do not hold."""
 
 import pytest
 import torch
@@ -45,4 +46,19 @@ def test_on_another_stream(S, handle):
         assert torch.equal(got[f].cpu(), want[f].cpu()), f
     assert layout["n_spans"].tolist() == seg["n_spans"].tolist()
     torch.cuda.synchronize()
+    assert ws.status() == 0
+
+
+@pytest.mark.parametrize("lens", [[700, 433], [433, 700]])
+def test_lengths_past_the_builder_are_refused(S, lens):
+    """A sequence longer than the builder's max_tokens, or of negative length, would lose tokens silently."""
+    c, bd, H, omega = _setup(S, lens, 699)
+    cache, ws = c.cache(S), c.workspace(S)
+    with pytest.raises(ValueError, match="max_tokens"):
+        S.build_layer_paged(bd, c.dims(S), cache, H, omega, ws)
+    cache.seq_len[lens.index(700)] = -1
+    with pytest.raises(ValueError, match="max_tokens"):
+        S.build_layer_paged(bd, c.dims(S), cache, H, omega, ws)
+    cache.seq_len[lens.index(700)] = 699
+    S.build_layer_paged(bd, c.dims(S), cache, H, omega, ws)
     assert ws.status() == 0
