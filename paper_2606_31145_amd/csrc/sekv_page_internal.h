@@ -1,4 +1,4 @@
-// Launch structures of the paged token store (sekv_page.hip, sekv_page_attend.h,
+// Launch structures of the paged token store (sekv_page.hip, sekv_page_attend_inst.hip,
 // sekv_page_api.cpp).
 #pragma once
 

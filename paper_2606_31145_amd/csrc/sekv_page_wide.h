@@ -152,8 +152,6 @@ struct Rows32 {
     f16v o[DB];
     float m, l;
     int lo, hi;                         // keys that the column's query sees
-    int lo_all, hi_all;                 // keys that every column sees
-    int lo_any, hi_any;                 // keys that some column sees
     int kaddr[QS], vaddr[2][DB];        // this lane's pieces in a tile
 
     __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane) {
@@ -161,15 +159,10 @@ struct Rows32 {
         const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
         int row = row0 + n;
         row = row < it.rows ? row : it.rows - 1;
-        const int last = row0 + 31 < it.rows ? row0 + 31 : it.rows - 1, first = row0 < it.rows ? row0 : it.rows - 1;
-        const int64_t p = it.p0 + (row >> gs), p_first = it.p0 + (first >> gs), p_last = it.p0 + (last >> gs), w = int64_t(a.window) - 1;
+        const int64_t p = it.p0 + (row >> gs), w = int64_t(a.window) - 1;
         auto cut = [&](int64_t x, int64_t top) { return int(x < -1 ? -1 : x < top ? x : top); };
         lo = cut(p - w < 0 ? 0 : p - w, cap);
         hi = cut(p, cap - 1);
-        lo_all = cut(p_last - w < 0 ? 0 : p_last - w, cap);
-        hi_all = cut(p_first, cap - 1);
-        lo_any = cut(p_first - w < 0 ? 0 : p_first - w, cap);
-        hi_any = row0 < it.rows ? cut(p_last, cap - 1) : -1;
         const uint16_t *src = static_cast<const uint16_t *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
                               ((g << gs) + (row & ((1 << gs) - 1))) * D;
 #pragma unroll
