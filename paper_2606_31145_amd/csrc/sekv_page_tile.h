@@ -24,6 +24,17 @@ typedef __bf16 b8v __attribute__((ext_vector_type(8)));
 
 constexpr float kSlack = 8.f;
 
+// A weight is exp2(score * scale_log2 - m) in one fused step, while m is the rounded product of the largest score: that
+// one's weight is 2 to the product's rounding error instead of 1.  The error is common to all weights and does no
+// harm while it is small.  Past kLargest it may be more than 4: such an item is done row by row instead, with
+// rounded products on both sides (plain_rows).  A maximum far below -kLargest that a later one replaced may have left
+// an infinite sum times zero, so a sum that is no number counts as well; where scores themselves are none, the
+// rows say so again.  Looked at once an item: a test at each new maximum cost 2048 tokens over 32768 keys 1 %.
+constexpr float kLargest = 67108864.f;
+__device__ inline int unsound(float m, float l) {            // without branches: those cost the loop before it registers
+    return (int(fabsf(m) > kLargest) & int(fabsf(m) < __builtin_inff())) | int(l != l);
+}
+
 __device__ inline f4v mma16(const uint4 &a, const uint4 &b, f4v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8v, a), __builtin_bit_cast(b8v, b), c, 0, 0, 0);
 }
@@ -580,7 +591,7 @@ struct Rows16 {
         }
     }
 
-    // Every step-th group of keys from pos on.  A group's keys and values are asked for as soon as the registers
+    // Every step-th group of keys from pos on.  bad: the item has to be done row by row.  A group's keys and values are asked for as soon as the registers
     // of an earlier one are free, kAhead groups ahead; its row blocks one group before that.  Two groups where they
     // fit: 32 ragged sequences in bfloat16 462 us against 469 with one, 4 of 131072 in 8 bits 188.6 against 191.2,
     // 13 of float and head_dim 64 577 against 599.
@@ -638,7 +649,7 @@ struct Rows16 {
     }
 };
 
-// An item whose masked keys hold infinities or NaN, row by row: a wave a row, 64 keys at a time, a
+// An item whose masked keys hold infinities or NaN, or whose scores are too large, row by row: a wave a row, 64 keys at a time, a
 // score a lane, then the values with the lanes over d.  Only keys that the row sees are touched.
 template <class T, class P, int D>
 __device__ inline void plain_rows(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave) {
