@@ -253,11 +253,8 @@ class Workspace:
         off = (-self._buf.data_ptr()) % 256
         self.tensor = self._buf[off:off + need]
         self.nbytes = need
-        _check(LIB.sekv_workspace_init(self.tensor.data_ptr(), need, _stream(stream)))
-
-    @property
-    def ptr(self) -> int:
-        return self.tensor.data_ptr()
+        self.ptr = self.tensor.data_ptr()
+        _check(LIB.sekv_workspace_init(self.ptr, need, _stream(stream)))
 
     def status(self, stream=None) -> int:
         bits = ctypes.c_int32(0)
