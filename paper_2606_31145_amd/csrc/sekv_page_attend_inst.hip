@@ -42,11 +42,9 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
     // the four waves' parts, joined through LDS
     float *ml = reinterpret_cast<float *>(lds), *so = ml + kWaves * 2 * N;
     const int n = lane & 15, gq = lane >> 4;
-    int odd = bad;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const float l = r.sum(nb);
-        odd |= unsound(r.m[nb], l);
         if (gq == 0) {
             ml[wave * 2 * N + 16 * nb + n] = r.m[nb];
             ml[wave * 2 * N + N + 16 * nb + n] = l;
@@ -56,7 +54,7 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
 #pragma unroll
             for (int e = 0; e < VE; ++e) so[(wave * N + 16 * nb + n) * RS + VE * (4 * gq + i) + e] = r.o[nb][e][i];
     }
-    if (__syncthreads_or(odd)) return true;
+    if (__syncthreads_or(bad)) return true;
     const int d0 = (threadIdx.x & 15) * 2;                   // and 32, 64, .. on: what 16 threads store lies together
     for (int rw = threadIdx.x >> 4; rw < it.rows; rw += 16) {
         float m = -INFINITY, sum = 0.f, o[VE / 2][2] = {};
@@ -88,12 +86,11 @@ __device__ inline bool wide_f32(const PageAttendArgs &a, const Item &it, int b, 
     using R = Rows16<F32, P, D, 2>;
     R r;
     bool bad = false;
-    r.m[0] = r.m[1] = r.l[0] = r.l[1] = 0.f;
     if (wave * 32 < it.rows) {
         r.init(a, it, g, wave * 32, lane);
         r.run(a, it, b, g, it.begin, 16, &bad, lane);
     }
-    if (__syncthreads_or(int(bad) | unsound(r.m[0], r.l[0]) | unsound(r.m[1], r.l[1]))) return true;
+    if (__syncthreads_or(bad)) return true;
     if (wave * 32 >= it.rows) return false;
     const int n = lane & 15, gq = lane >> 4;
 #pragma unroll
@@ -203,7 +200,7 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     };
     if (it.begin < it.end)
         while (turn(std::integral_constant<int, 0>{}) && turn(std::integral_constant<int, 1>{})) {}
-    if (__syncthreads_or(int(bad) | unsound(r.m, r.l))) return true;
+    if (__syncthreads_or(int(bad) | int(too_large(r.m)))) return true;
     const int n = lane & 31, h = lane >> 5, rw = wave * 32 + n;
     const float l = r.l + across32(r.l);
     if (rw < it.rows) {

@@ -26,13 +26,11 @@ constexpr float kSlack = 8.f;
 
 // A weight is exp2(score * scale_log2 - m) in one fused step, while m is the rounded product of the largest score: that
 // one's weight is 2 to the product's rounding error instead of 1.  The error is common to all weights and does no
-// harm while it is small.  Past kLargest it may be more than 4: such an item is done row by row instead, with
-// rounded products on both sides (plain_rows).  A maximum far below -kLargest that a later one replaced may have left
-// an infinite sum times zero, so a sum that is no number counts as well; where scores themselves are none, the
-// rows say so again.  Looked at once an item: a test at each new maximum cost 2048 tokens over 32768 keys 1 %.
+// harm while it is small.  Past kLargest it may be more than 4: an item that meets such a maximum is done row by row
+// instead, with rounded products on both sides (plain_rows).  Infinite maxima make no number either way.
 constexpr float kLargest = 67108864.f;
-__device__ inline int unsound(float m, float l) {            // without branches: those cost the loop before it registers
-    return (int(fabsf(m) > kLargest) & int(fabsf(m) < __builtin_inff())) | int(l != l);
+__device__ inline bool too_large(float m) {                  // kLargest < |m| < infinity, without branches
+    return (__float_as_uint(m) & 0x7fffffffu) - 0x4c800001u < 0x7f800000u - 0x4c800001u;
 }
 
 __device__ inline f4v mma16(const uint4 &a, const uint4 &b, f4v c) {
@@ -461,8 +459,8 @@ struct Rows16 {
     }
 
     // Mask, running maximum and weights of the keys from pos on; valid: a bit for each block that holds
-    // keys.  True when some column does not see some key.
-    __device__ bool weights(const PageAttendArgs &a, f4v (&s)[J][NB], int pos, uint32_t valid, int lane) {
+    // keys.  True when some column does not see some key.  bad: the maximum is too large.
+    __device__ bool weights(const PageAttendArgs &a, f4v (&s)[J][NB], int pos, uint32_t valid, bool *bad, int lane) {
         const int g = lane >> 4;
         const bool part = valid != (1u << J) - 1 || pos < lo_all || pos + Tile::kKeys - 1 > hi_all;
         if (part) {
@@ -495,6 +493,7 @@ struct Rows16 {
                 const float mn = fmaxf(m[nb], x);
                 const float f = exp2_fast(m[nb] - (mn == -INFINITY ? 0.f : mn));
                 m[nb] = mn;
+                *bad |= too_large(mn);
                 l[nb] *= f;
 #pragma unroll
                 for (int e = 0; e < VE; ++e) o[nb][e] *= f;
@@ -591,10 +590,10 @@ struct Rows16 {
         }
     }
 
-    // Every step-th group of keys from pos on.  bad: the item has to be done row by row.  A group's keys and values are asked for as soon as the registers
-    // of an earlier one are free, kAhead groups ahead; its row blocks one group before that.  Two groups where they
-    // fit: 32 ragged sequences in bfloat16 462 us against 469 with one, 4 of 131072 in 8 bits 188.6 against 191.2,
-    // 13 of float and head_dim 64 577 against 599.
+    // Every step-th group of keys from pos on.  bad: the item has to be done row by row.
+    // A group's keys and values are asked for as soon as the registers of an earlier one are free, kAhead groups
+    // ahead; its row blocks one group before that.  Two groups where they fit: 32 ragged sequences in bfloat16 462 us
+    // against 469 with one, 4 of 131072 in 8 bits 188.6 against 191.2, 13 of float and head_dim 64 577 against 599.
     static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW), kHeld = NB * (D / 4 + QW);
     static constexpr int kAhead = 2 * kTileWords + kHeld <= 176 ? 2 : 1;      // of 256 registers
     __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int step, bool *bad, int lane) {
@@ -620,7 +619,7 @@ struct Rows16 {
                 f4v s[J][NB];
                 scores(t[u], s);
                 if (more) t[u].load_keys(a, row, lane);
-                const bool part = weights(a, s, pos, valid[u], lane);
+                const bool part = weights(a, s, pos, valid[u], bad, lane);
                 values(t[u], s, pos, valid[u], part, bad, lane);
                 if (more) {
                     t[u].load_values(a, row, lane);
@@ -649,8 +648,8 @@ struct Rows16 {
     }
 };
 
-// An item whose masked keys hold infinities or NaN, or whose scores are too large, row by row: a wave a row, 64 keys at a time, a
-// score a lane, then the values with the lanes over d.  Only keys that the row sees are touched.
+// An item whose masked keys hold infinities or NaN, or whose scores are too large, row by row: a wave a row, 64
+// keys at a time, a score a lane, then the values with the lanes over d.  Only keys that the row sees are touched.
 template <class T, class P, int D>
 __device__ inline void plain_rows(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave) {
     auto element = [](const void *pool, const uint8_t *scale, int row, int i) {

@@ -145,6 +145,10 @@ struct Direct {
     }
 };
 
+// A maximum that is too large (sekv_page_tile.h) is put where no finite score moves it, and found there at the end.
+// A flag beside it cost 2048 tokens over 32768 keys 1 %.
+constexpr float kTooLarge = 3e38f;
+
 template <int D>
 struct Rows32 {
     static constexpr int DB = D / 32, QS = D / 16;
@@ -228,7 +232,8 @@ struct Rows32 {
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
         if (__any(mx * a.scale_log2 > m + kSlack)) {
             const float x = fmaxf(mx, across32(mx)) * a.scale_log2;
-            const float mn = fmaxf(m, x);
+            float mn = fmaxf(m, x);
+            mn = too_large(mn) ? kTooLarge : mn;
             const float f = exp2_fast(m - (mn == -INFINITY ? 0.f : mn));
             m = mn;
             l *= f;

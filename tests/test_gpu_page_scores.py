@@ -81,6 +81,38 @@ def test_scores_of_any_size(S, dtype, store, lens, news, group, dim, scale, sign
 
 @pytest.mark.parametrize("dtype,store", STORES)
 @pytest.mark.parametrize("news,group", [([1, 1], 4), ([20, 6], 4), ([150, 33], 1)])
+@pytest.mark.parametrize("low", [-1e5, -3e8, -1e10, -1e20])
+def test_a_maximum_far_below_the_next(S, dtype, store, news, group, low):
+    """The first 200 keys' scores are far below the others': they weigh nothing, whatever their own sums were."""
+    c = Case(dtype, store, [900, 477], news, kv_heads=2, group=group, dim=128, page=16, scale=1.0,
+             seed=zlib.crc32(repr((dtype, store, news, low)).encode()))
+    g = torch.Generator().manual_seed(6)
+    for b in range(2):
+        p, s = c.rows(b)
+        x = torch.zeros((c.lens[b], c.Hkv, c.d), dtype=torch.float64)
+        x[..., 0] = torch.randint(-4, 5, x.shape[:-1], generator=g).double()
+        x[:200, :, 0] = low * torch.randint(1, 3, (200, c.Hkv), generator=g).double()
+        if store == "e4m3":
+            codes, e = encode_rows(x)
+            c.codes["k"][0][p, :, s], c.codes["k"][1][p, :, s] = codes, e
+            c.pools["k"][p, :, s] = decode_rows(codes, e)
+        else:
+            c.codes["k"][0][p, :, s] = x.to(c.codes["k"][0].dtype)
+            c.pools["k"][p, :, s] = c.codes["k"][0][p, :, s].double()
+    c.q = torch.zeros_like(c.q)
+    c.q[..., 0] = 1.0
+    cache, ws = c.cache(S), c.workspace(S)
+    out, lse = (t.cpu().double() for t in S.page_attend(c.dims(S), cache, c.q.cuda(), c.tok_start(), ws, want_lse=True))
+    ref, z, size, _ = _reference(c)
+    half, n = HALF_STEP[dtype], 900
+    # scores of at most 4: arguments within 6 * 2^-23, then exp2, sums, division as above
+    err = 12 * 2.0 ** -23 + 2 * n * 2.0 ** -24 + 2.0 ** -22 + (half if dtype == "bf16" else 0.0)
+    assert ((out - ref).abs() <= 1.01 * (err * size + half * ref.abs()) + 1e-38).all() and ws.status() == 0
+    assert ((lse - z).abs() <= 2.0 ** -21 * z.abs().clamp(min=1) + 6 * 2.0 ** -23 + (n + 4) * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("dtype,store", STORES)
+@pytest.mark.parametrize("news,group", [([1, 1], 4), ([20, 6], 4), ([150, 33], 1)])
 @pytest.mark.parametrize("spread", [1e6, 1e10, 1e15])
 def test_large_queries(S, dtype, store, news, group, spread):
     """Queries far outside any softmax's usual range: the results stay averages of values."""
