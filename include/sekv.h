@@ -419,7 +419,8 @@ SEKV_API sekv_status sekv_page_read(const sekv_page_dims *dims, const sekv_pages
  * unless NULL, lse float [n_tokens][Hq], the natural logarithm of the softmax's denominator.
  * A query that sees nothing (position below 0), or whose scores are all -inf, gets zeros and
  * -inf.  Keys and values that a query does not see do not reach it, whatever they hold.
- * Scores and sums are held in float; with bfloat16 tokens the softmax weights are rounded to
+ * Scores, and sums of values weighted by up to 2^8, are held in float (an item whose scores pass 2^26 in
+ * magnitude is done row by row, some 300 times slower); with bfloat16 tokens the softmax weights are rounded to
  * bfloat16 for the matrix cores (off by at most 2^-8 of each); with float tokens nothing is. */
 SEKV_API sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages, const void *q,
                                       int64_t q_stride, const int32_t *tok_start, int32_t n_tokens,

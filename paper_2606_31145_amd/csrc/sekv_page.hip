@@ -150,8 +150,9 @@ __device__ inline void store_row(const PageAppendArgs &a, int side, int to, cons
 // tokens are consecutive rows of a page, so that what a workgroup writes, exponent bytes included, lies
 // together.  A row belongs to L lanes of 16 bytes, keys and values side by side.  The rows are asked for
 // before their places are looked up, and stored past the caches: they are read again only with everything
-// stored before them.  Four 8192-token chunks of 8 heads in 8 bits (202 MB): 51.4 us with plain stores and
-// four tokens a thread, 42.0 with stores past the caches, 38.1 with one token a thread as well (two: 39.5).
+// stored before them.  Four 8192-token chunks of 8 heads in 8 bits (202 MB), two sets of inputs in turn, which
+// the last-level cache partly holds: 51.4 us with plain stores and four tokens a thread, 42.0 with stores past the
+// caches, 38.1 with one token a thread as well (two: 39.5).  With inputs from memory it is 42.0 (4.8 TB/s).
 template <class T, class P, int D>
 __global__ void __launch_bounds__(kThreads) append_kernel(PageAppendArgs a) {
     constexpr int L = D / Piece<T>::kN, kRows = kThreads / L;

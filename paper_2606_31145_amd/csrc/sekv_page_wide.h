@@ -9,8 +9,8 @@
 // straight into LDS, 8-bit codes through registers, where they become scaled bfloat16, so that the rest
 // knows one type only.
 //
-// Measured, 2048 tokens over 32768 keys, head_dim 128, bfloat16 (1065 GFLOP): 1055 us, 1009 TFLOP/s, where a
-// 16384^3 matrix product reaches 1364; in 8 bits 1081 us; head_dim 64 665 us.  The matrix cores are busy for 48 %
+// Measured, 2048 tokens over 32768 keys, head_dim 128, bfloat16 (1065 GFLOP): 1060 to 1120 us by the card, 951 to
+// 1005 TFLOP/s, where a 16384^3 matrix product reaches 1364; in 8 bits 1081 us; head_dim 64 665 us.  The matrix cores are busy for 48 %
 // of the cycles, at a clock that the load brings down to 1.95 GHz.  The way there: 1211 us with the blocks of a
 // tile looked up by one lane each instead of by all, 1166; the LDS reads placed among the products
 // (sched_group_barrier) 1146; bfloat16 straight into LDS 1067.  No gain came from a priority for half of
@@ -198,6 +198,9 @@ struct Rows32 {
 
     // One tile: 64 keys from pos on.  part: some column may not see some key, and `valid` says which of the
     // four blocks hold keys.  The sum takes the weights before they are rounded: lse is a float.
+    // The products take them in bfloat16, beside values of that type: 2048 tokens over 32768 keys are 1.98e-3 off 64
+    // bits (root mean square, relative), 1.65e-3 of it the output's own rounding.  A second product with what the
+    // rounding left would add half as many matrix instructions again.
     __device__ void step(const PageAttendArgs &a, lds_bytes kt, lds_bytes vt, int pos, uint32_t valid, bool part, int lane) {
         const int h = lane >> 5;
         f16v s[2];

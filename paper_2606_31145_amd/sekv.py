@@ -753,7 +753,8 @@ class PageCache:
 
     def struct(self, pd: PageDims) -> PagesStruct:
         """The C view.  Types, sizes and devices are checked against pd when an attribute was set, a
-        tensor has moved or pd is another than in the last call."""
+        tensor has moved or pd is another than in the last call.  A tensor's shape and strides are not to
+        be changed in place meanwhile: set the attribute instead."""
         seen = (bytes(pd), *[None if x is None else x.data_ptr() for x in self._tensors()])
         if seen == self._seen:
             return self._struct
@@ -856,7 +857,8 @@ def page_read(pd: PageDims, cache: PageCache, max_tokens: int, ws: Workspace, ke
 def page_attend(pd: PageDims, cache: PageCache, q, tok_start, ws: Workspace, out=None, lse=None,
                 want_lse: bool = False, stream=None):
     """sekv_page_attend: (out [n_tokens][Hq][d], lse float [n_tokens][Hq] or None) of the queries
-    q [n_tokens][Hq][d] (tokens may be strided)."""
+    q [n_tokens][Hq][d] (tokens may be strided); rows that belong to no sequence are left as given,
+    undefined in tensors allocated here."""
     cs, dev = cache.struct(pd), cache.k_pages.device
     qp, sq = _token_rows(pd, q, "q", pd.n_q_heads, dev)
     ts = _tok_start(pd, tok_start, dev)
