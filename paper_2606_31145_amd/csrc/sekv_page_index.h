@@ -214,9 +214,9 @@ SEKV_HD int64_t partial_rows(int n_tokens, int Hkv, int group_shift, int64_t cap
 // leaves a tile of 128 rows to one compute unit, so it is for tiles that are probably narrow; more rows
 // than sequences of narrow tiles hold mean that some tile is not.  Fewer do not mean that none is: a chunk beside
 // many single tokens is joined in the last workgroups of its 128-row tiles, too, for the whole call goes one way.
-// Measured (us), joined in the last workgroup and by a second kernel: one token over 2048 float keys 10.4, 12.3, of 8 sequences at 9001 in 8 bits 30.5, 36.0,
-// six of 16 under a window of 4096 30.9, 35.5; 257 over 9001 90.8, 60.6, 13 ragged sequences, one of 257
-// tokens, 117.7, 90.3, two of 333 in float 75.3, 58.0; 8 heads at 9000 keys in 8 bits, 128 ragged single tokens at
+// Measured (us), joined in the last workgroup and by a second kernel: one token over 2048 float keys 10.4, 12.3,
+// of 8 sequences at 9001 in 8 bits 30.5, 36.0, six of 16 under a window of 4096 30.9, 35.5; 257 over 9001 90.8, 60.6,
+// 13 ragged sequences, one of 257 tokens, 117.7, 90.3, two of 333 in float 75.3, 58.0; 8 heads at 9000 keys in 8 bits, 128 ragged single tokens at
 // 2000 85.9, 116.8, 31 and a chunk of 257 203.8, 190.3, 31 and one of 480 222.6, 237.7, 63 and one of 512 383.3, 376.3;
 // in bfloat16 140.0, 174.0; 283.8, 275.8; 305.4, 352.6; 541.9, 539.9.
 SEKV_HD bool join_in_launch(int batch, int n_tokens, int group_shift) {

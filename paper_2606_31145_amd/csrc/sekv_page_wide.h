@@ -10,9 +10,9 @@
 // knows one type only.
 //
 // Measured, 2048 tokens over 32768 keys, head_dim 128, bfloat16 (1065 GFLOP): 1060 to 1120 us by the card, 951 to
-// 1005 TFLOP/s, where a 16384^3 matrix product reaches 1364; in 8 bits 1081 us; head_dim 64 665 us.  The matrix cores are busy for 48 %
-// of the cycles, at a clock that the load brings down to 1.95 GHz.  The way there: 1211 us with the blocks of a
-// tile looked up by one lane each instead of by all, 1166; the LDS reads placed among the products
+// 1005 TFLOP/s, where a 16384^3 matrix product reaches 1364; in 8 bits 1081 us; head_dim 64 665 us.
+// The matrix cores are busy for 48 % of the cycles, at a clock that the load brings down to 1.95 GHz.
+// The way there: 1211 us with the blocks of a tile looked up by one lane each instead of by all, 1166; the LDS reads placed among the products
 // (sched_group_barrier) 1146; bfloat16 straight into LDS 1067.  No gain came from a priority for half of
 // the waves (1109 against 1101), nor from starting a tile's scores before the last one's values (1126 to
 // 1172 against 1124).  In copies that leave work out, the products alone take 688 us; without the exponentials it
