@@ -9,7 +9,7 @@
 // straight into LDS, 8-bit codes through registers, where they become scaled bfloat16, so that the rest
 // knows one type only.
 //
-// Measured, 2048 tokens over 32768 keys, head_dim 128, bfloat16 (1065 GFLOP): 1060 to 1120 us by the card, 951 to
+// Measured, 2048 tokens over 32768 keys, head_dim 128, bfloat16 (1065 GFLOP): 1060 to 1150 us by the card, 925 to
 // 1005 TFLOP/s, where a 16384^3 matrix product reaches 1364; in 8 bits 1081 us; head_dim 64 665 us.
 // The matrix cores are busy for 48 % of the cycles, at a clock that the load brings down to 1.95 GHz.
 // The way there: 1211 us with the blocks of a tile looked up by one lane each instead of by all, 1166; the LDS reads placed among the products
