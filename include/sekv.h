@@ -71,7 +71,8 @@ typedef enum {
     SEKV_ERR_HIP = 4            /* a HIP runtime call failed; see sekv_last_error()  */
 } sekv_status;
 
-typedef enum { SEKV_F32 = 0, SEKV_BF16 = 1, SEKV_E4M3 = 2 /* page storage only */ } sekv_dtype;
+/* E4M3 and E2M1: page storage only */
+typedef enum { SEKV_F32 = 0, SEKV_BF16 = 1, SEKV_E4M3 = 2, SEKV_E2M1 = 3 } sekv_dtype;
 
 /* Implementation choice for the zoomed spans (sekv_dims.flags bits 0..1). */
 #define SEKV_ZOOM_DEFAULT 0     /* library default (currently FACTORED)                     */
@@ -344,6 +345,14 @@ SEKV_API sekv_status sekv_build_cache(const sekv_build_dims *dims, const void *k
  * an e4m3 step (2^-4 of it, or 2^-10 * 2^(E - 127) for the smallest); read back in dims.dtype
  * it is exact again (but for values beyond that type: those that were rounded up past its largest,
  * and subnormal ones).  Infinities and NaN are stored as NaN in 8 bits.
+ * Or (page_dtype = SEKV_E2M1) as 4 bits a value, two a byte with the earlier one in the low half, and
+ * one exponent byte for every 32 values of a row:
+ *   value = code * 2^(E - 127), code one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 or its negative (sign, 2 bits of
+ *   exponent, 1 of mantissa), E the smallest exponent of 2 .. 252 with max |x| <= 6 * 2^(E - 127) over the
+ *   block; E = 127 for a block of zeros.
+ * A stored value is off by at most half a step of its code (a quarter of it, 2^-2 * 2^(E - 127) for the
+ * smallest; values past 6 * 2^125 become that) and read back in dims.dtype it is exact.  A block that holds
+ * an infinity or NaN has E = 255, which reads as NaN throughout.
  *
  * Ragged batches: the new tokens of all sequences lie one after another; sequence b has rows
  * tok_start[b] .. tok_start[b + 1] - 1 of n_tokens (tok_start int32 [B + 1], never descending, within 0 and
@@ -370,7 +379,7 @@ typedef struct {
     int32_t n_pages;        /* pages in the pool, n_pages * Hkv * page_size < 2^31         */
     int32_t max_pages;      /* row stride of the page table, max_pages * page_size <= 2^30 */
     int32_t dtype;          /* SEKV_F32 or SEKV_BF16: new tokens, queries, outputs          */
-    int32_t page_dtype;     /* dtype, or SEKV_E4M3                                         */
+    int32_t page_dtype;     /* dtype, SEKV_E4M3 or SEKV_E2M1                               */
     int32_t window;         /* a query sees at most this many keys, its own last; 0: all   */
     int32_t reserved[2];    /* 0                                                           */
     double softmax_scale;   /* in [1e-30, 1e30]                                            */
@@ -378,9 +387,10 @@ typedef struct {
 
 /* One layer's pages.  Device pointers, caller-owned; pools and scales 16-byte aligned. */
 typedef struct {
-    void *k;                /* [n_pages][Hkv][page_size][d] in page_dtype                  */
+    void *k;                /* [n_pages][Hkv][page_size][d] in page_dtype (E2M1: d / 2 bytes)  */
     void *v;
-    uint8_t *k_scale;       /* [n_pages][Hkv][page_size] exponents E; NULL unless E4M3     */
+    uint8_t *k_scale;       /* exponents E, [n_pages][Hkv][page_size] for E4M3, that and [d / 32] for
+                               E2M1, else NULL                                             */
     uint8_t *v_scale;
     const int32_t *table;   /* [B][max_pages]                                              */
     const int32_t *seq_len; /* [B]                                                         */

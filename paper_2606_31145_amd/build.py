@@ -29,7 +29,8 @@ DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", f"-I{INCLUDE}", f"-I{CSRC}"]
 SVD_INSTANCES = [(2, 128), (4, 128), (2, 64), (4, 64)]      # (element bytes, head_dim)
 PAGE_INSTANCES = [("BF16", "BF16", 128), ("BF16", "E4M3", 128), ("BF16", "BF16", 64), ("BF16", "E4M3", 64),
-                  ("F32", "F32", 128), ("F32", "E4M3", 128), ("F32", "F32", 64), ("F32", "E4M3", 64)]
+                  ("F32", "F32", 128), ("F32", "E4M3", 128), ("F32", "F32", 64), ("F32", "E4M3", 64),
+                  ("BF16", "E2M1", 128), ("BF16", "E2M1", 64), ("F32", "E2M1", 128), ("F32", "E2M1", 64)]
 INSTANCES = [("BF16", 128), ("BF16", 64), ("F32", 128), ("F32", 64)]
 
 # every source the kernels are built from (the bench hashes these to tie counter

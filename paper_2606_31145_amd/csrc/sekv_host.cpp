@@ -325,7 +325,7 @@ sekv_status check_page_dims(const sekv_page_dims *d) {
         return fail(SEKV_ERR_UNSUPPORTED, "max_pages %d too large", d->max_pages);
     if (d->dtype != SEKV_F32 && d->dtype != SEKV_BF16)
         return fail(SEKV_ERR_UNSUPPORTED, "dtype %d", d->dtype);
-    if (d->page_dtype != d->dtype && d->page_dtype != SEKV_E4M3)
+    if (d->page_dtype != d->dtype && d->page_dtype != SEKV_E4M3 && d->page_dtype != SEKV_E2M1)
         return fail(SEKV_ERR_UNSUPPORTED, "page_dtype %d with dtype %d", d->page_dtype, d->dtype);
     if (d->window < 0) return fail(SEKV_ERR_INVALID_ARG, "window < 0");
     if (d->reserved[0] != 0 || d->reserved[1] != 0)
@@ -345,10 +345,10 @@ sekv_status check_pages(const sekv_page_dims *d, const sekv_pages *p) {
         return fail(SEKV_ERR_INVALID_ARG, "page pools not 16-byte aligned");
     if (misaligned(p->table, 4) || misaligned(p->seq_len, 4))
         return fail(SEKV_ERR_INVALID_ARG, "page table or seq_len not 4-byte aligned");
-    const bool e4m3 = d->page_dtype == SEKV_E4M3;
-    if (e4m3 && (!p->k_scale || !p->v_scale))
+    const bool scaled = d->page_dtype == SEKV_E4M3 || d->page_dtype == SEKV_E2M1;
+    if (scaled && (!p->k_scale || !p->v_scale))
         return fail(SEKV_ERR_INVALID_ARG, "pages.k_scale or v_scale is NULL");
-    if (!e4m3 && (p->k_scale || p->v_scale))
+    if (!scaled && (p->k_scale || p->v_scale))
         return fail(SEKV_ERR_INVALID_ARG, "scales given for pages without them");
     if (misaligned(p->k_scale, 16) || misaligned(p->v_scale, 16))
         return fail(SEKV_ERR_INVALID_ARG, "page scales not 16-byte aligned");

@@ -22,6 +22,10 @@ hipError_t launch_page_attend_F32_F32_128(const PageAttendArgs &a, hipStream_t s
 hipError_t launch_page_attend_F32_F32_64(const PageAttendArgs &a, hipStream_t s);
 hipError_t launch_page_attend_F32_E4M3_128(const PageAttendArgs &a, hipStream_t s);
 hipError_t launch_page_attend_F32_E4M3_64(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_BF16_E2M1_128(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_BF16_E2M1_64(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_F32_E2M1_128(const PageAttendArgs &a, hipStream_t s);
+hipError_t launch_page_attend_F32_E2M1_64(const PageAttendArgs &a, hipStream_t s);
 
 namespace {
 
@@ -31,20 +35,20 @@ constexpr int kThreads = 256;
 constexpr int64_t kMaxBlocks = 1 << 21;   // a launch stays below 2^32 threads
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
-// The largest of L lanes' words, in each of them (L = 8, 16, 32; a group of lanes starts at a multiple of L).
+// The largest of L lanes' words, in each of them (L = 4, 8, 16, 32; a group of lanes starts at a multiple of L).
 template <int L>
 __device__ inline uint32_t lanes_max(uint32_t x) {
     auto with = [&](uint32_t y) { x = x > y ? x : y; };
     with(__builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true));       // quad_perm: lane ^ 1
     with(__builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true));       // quad_perm: lane ^ 2
-    with(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));      // 7 - lane of 8
+    if constexpr (L >= 8) with(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));    // 7 - lane of 8
     if constexpr (L >= 16) with(__builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));   // 15 - lane of 16
     if constexpr (L >= 32) with(__shfl_xor(x, 16));
     return x;
 }
 
 // 16 bytes of a row: as floats; the bits of the largest magnitude as a float's (an infinity's or NaN's if there
-// is one); four of its values as codes, scaled by the power of two.
+// is one); four of its values as 8-bit codes, all of them as 4-bit codes, scaled by the power of two.
 template <class T> struct Piece;
 template <> struct Piece<F32> {
     static constexpr int kN = 4;
@@ -55,6 +59,10 @@ template <> struct Piece<F32> {
         const uint32_t a = w[0] & 0x7fffffffu, b = w[1] & 0x7fffffffu, c = w[2] & 0x7fffffffu, d = w[3] & 0x7fffffffu;
         const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
         return ab > cd ? ab : cd;
+    }
+    static __device__ uint32_t codes4(const u4v &w, float scale) {
+        const uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(w[0]), __uint_as_float(w[1]), scale, 0);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(w[2]), __uint_as_float(w[3]), scale, 1);
     }
     static __device__ uint32_t codes(const u4v &w, int, float scale) {
         typedef short s2v __attribute__((ext_vector_type(2)));
@@ -78,6 +86,14 @@ template <> struct Piece<BF16> {
         auto h = [&](int i) { return __builtin_bit_cast(h2v, w[i] & 0x7fff7fffu); };
         const h2v m = __builtin_elementwise_max(__builtin_elementwise_max(h(0), h(1)), __builtin_elementwise_max(h(2), h(3)));
         return uint32_t(m[0] > m[1] ? m[0] : m[1]) << 16;
+    }
+    static __device__ uint32_t codes4(const u4v &w, float scale) {
+        typedef __bf16 b2v __attribute__((ext_vector_type(2)));
+        const uint32_t a = w[0], b = w[1], c = w[2], d = w[3];   // a bit cast of w[k] itself takes element 0
+        uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(b2v, a), scale, 0);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(b2v, b), scale, 1);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(b2v, c), scale, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(b2v, d), scale, 3);
     }
     static __device__ uint32_t codes(const u4v &w, int i, float scale) {
         typedef short s2v __attribute__((ext_vector_type(2)));
@@ -110,6 +126,14 @@ __device__ inline void store_row(const PageAppendArgs &a, int side, int to, cons
     constexpr int N = Piece<T>::kN, L = D / N;
     if constexpr (P::kBytes == T::kBytes) {
         __builtin_nontemporal_store(w, reinterpret_cast<u4v *>(static_cast<unsigned char *>(a.pool[side]) + size_t(to) * (D * T::kBytes)) + lane);
+    } else if constexpr (P::kBytes == 0) {
+        constexpr int LB = P::kBlock / N;                    // lanes of a block
+        const uint32_t Ex = block_exponent(lanes_max<LB>(Piece<T>::top(w)));
+        const uint32_t c = Piece<T>::codes4(w, pow2_of(Ex));
+        unsigned char *dst = static_cast<unsigned char *>(a.pool[side]) + size_t(to) * P::row(D) + lane * (N / 2);
+        if constexpr (N == 8) __builtin_nontemporal_store(c, reinterpret_cast<uint32_t *>(dst));
+        else __builtin_nontemporal_store(uint16_t(c), reinterpret_cast<uint16_t *>(dst));
+        if (lane % LB == 0) a.scale[side][size_t(to) * P::scales(D) + lane / LB] = uint8_t(Ex);
     } else {
         uint32_t c[N / 4];
         float m = __uint_as_float(lanes_max<L>(Piece<T>::top(w)));
@@ -209,6 +233,20 @@ template <> struct Stored<F32, E4M3> {
     }
 };
 
+template <> struct Stored<BF16, E2M1> {
+    using W = uint32_t;
+    static __device__ u4v up(const W &w, float scale) { return __builtin_bit_cast(u4v, word_bf16(w, scale)); }
+};
+template <> struct Stored<F32, E2M1> {
+    using W = uint16_t;
+    static __device__ u4v up(const W &w, float scale) {
+        float x[4];
+        pair_f32<0>(w, scale, x[0], x[1]);
+        pair_f32<1>(w, scale, x[2], x[3]);
+        return u4v{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+    }
+};
+
 // 64 tokens of one sequence and head for a workgroup, 16 of them (one block, in one page) for a wave, whose
 // rows are consecutive on both sides.  A lane takes what makes 16 bytes of the dense side, which is the larger:
 // four sequences of 131072 in 8 bits to bfloat16 (3.2 GB) 612 us (5.3 TB/s, a copy 5.1) against 676 with 16 bytes
@@ -238,8 +276,8 @@ __global__ void __launch_bounds__(kThreads) read_kernel(PageReadArgs a) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 w[s][i] = reinterpret_cast<const typename S::W *>(static_cast<const unsigned char *>(a.pool[s]) +
-                                                                  size_t(from) * (D * P::kBytes))[i * 64 + lane];
-                E[s][i] = P::kBytes == 1 ? a.scale[s][from + (i * 64 + lane) / PC] : 127u;
+                                                                  size_t(from) * P::row(D))[i * 64 + lane];
+                E[s][i] = P::scales(D) ? a.scale[s][size_t(from) * P::scales(D) + (i * 64 + lane) * P::scales(D) / PC] : 127u;
             }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -271,15 +309,18 @@ hipError_t read(const PageReadArgs &a, hipStream_t s) {
 }
 
 // f(storage types, head_dim) for the combinations that check_page_dims lets through
+template <class T, class F>
+hipError_t dispatch_storage(int page_dtype, F f) {
+    if (page_dtype == SEKV_E4M3) return f(T{}, E4M3{});
+    if (page_dtype == SEKV_E2M1) return f(T{}, E2M1{});
+    return f(T{}, T{});
+}
 template <class F>
 hipError_t dispatch(int dtype, int page_dtype, int d, F f) {
-    const bool q = page_dtype == SEKV_E4M3;
-    if (dtype == SEKV_BF16) {
-        if (d == 128) return q ? f(BF16{}, E4M3{}, std::integral_constant<int, 128>{}) : f(BF16{}, BF16{}, std::integral_constant<int, 128>{});
-        return q ? f(BF16{}, E4M3{}, std::integral_constant<int, 64>{}) : f(BF16{}, BF16{}, std::integral_constant<int, 64>{});
-    }
-    if (d == 128) return q ? f(F32{}, E4M3{}, std::integral_constant<int, 128>{}) : f(F32{}, F32{}, std::integral_constant<int, 128>{});
-    return q ? f(F32{}, E4M3{}, std::integral_constant<int, 64>{}) : f(F32{}, F32{}, std::integral_constant<int, 64>{});
+    auto with_d = [&](auto t, auto p) {
+        return d == 128 ? f(t, p, std::integral_constant<int, 128>{}) : f(t, p, std::integral_constant<int, 64>{});
+    };
+    return dtype == SEKV_BF16 ? dispatch_storage<BF16>(page_dtype, with_d) : dispatch_storage<F32>(page_dtype, with_d);
 }
 
 }  // namespace
@@ -300,13 +341,14 @@ hipError_t launch_page_read(const PageReadArgs &a, int dtype, int page_dtype, in
 }
 
 hipError_t launch_page_attend(const PageAttendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t s) {
-    const bool q = page_dtype == SEKV_E4M3;
     if (dtype == SEKV_BF16) {
-        if (head_dim == 128) return q ? launch_page_attend_BF16_E4M3_128(a, s) : launch_page_attend_BF16_BF16_128(a, s);
-        return q ? launch_page_attend_BF16_E4M3_64(a, s) : launch_page_attend_BF16_BF16_64(a, s);
+        if (page_dtype == SEKV_E2M1) return head_dim == 128 ? launch_page_attend_BF16_E2M1_128(a, s) : launch_page_attend_BF16_E2M1_64(a, s);
+        if (page_dtype == SEKV_E4M3) return head_dim == 128 ? launch_page_attend_BF16_E4M3_128(a, s) : launch_page_attend_BF16_E4M3_64(a, s);
+        return head_dim == 128 ? launch_page_attend_BF16_BF16_128(a, s) : launch_page_attend_BF16_BF16_64(a, s);
     }
-    if (head_dim == 128) return q ? launch_page_attend_F32_E4M3_128(a, s) : launch_page_attend_F32_F32_128(a, s);
-    return q ? launch_page_attend_F32_E4M3_64(a, s) : launch_page_attend_F32_F32_64(a, s);
+    if (page_dtype == SEKV_E2M1) return head_dim == 128 ? launch_page_attend_F32_E2M1_128(a, s) : launch_page_attend_F32_E2M1_64(a, s);
+    if (page_dtype == SEKV_E4M3) return head_dim == 128 ? launch_page_attend_F32_E4M3_128(a, s) : launch_page_attend_F32_E4M3_64(a, s);
+    return head_dim == 128 ? launch_page_attend_F32_F32_128(a, s) : launch_page_attend_F32_F32_64(a, s);
 }
 
 }  // namespace sekv

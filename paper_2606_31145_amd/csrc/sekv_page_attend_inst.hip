@@ -18,7 +18,7 @@
 #include "sekv_page_wide.h"
 
 #if !defined(SEKV_T) || !defined(SEKV_P) || !defined(SEKV_D)
-#error "build with -DSEKV_T=BF16|F32 -DSEKV_P=BF16|F32|E4M3 -DSEKV_D=64|128"
+#error "build with -DSEKV_T=BF16|F32 -DSEKV_P=BF16|F32|E4M3|E2M1 -DSEKV_D=64|128"
 #endif
 
 namespace sekv {
@@ -131,7 +131,7 @@ __device__ inline bool wide_bf16(const PageAttendArgs &a, const Item &it, int b,
     const int64_t w = it.p0 + it.n_tok - 1 - (int64_t(a.window) - 1);
     const int64_t all_lo = w, all_hi = it.p0;                // keys that every row of the item sees
     constexpr bool kDirect = P::kBytes == 2;
-    Stage<D> st;
+    Stage<P, D> st;
     Direct<D> dr;
     bool bad = false;
     // everybody's part of a tile is in LDS

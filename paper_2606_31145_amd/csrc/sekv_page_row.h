@@ -10,10 +10,29 @@
 namespace sekv {
 namespace page {
 
-// Storage forms as template arguments.
-struct F32 { using elem = float; static constexpr int kBytes = 4; };
-struct BF16 { using elem = uint16_t; static constexpr int kBytes = 2; };
-struct E4M3 { using elem = uint8_t; static constexpr int kBytes = 1; };
+// Storage forms as template arguments: bytes of a value (0: two values a byte), of a row, and a row's exponent bytes.
+struct F32 {
+    using elem = float;
+    static constexpr int kBytes = 4;
+    static constexpr int row(int d) { return 4 * d; }
+    static constexpr int scales(int) { return 0; }
+};
+struct BF16 {
+    using elem = uint16_t;
+    static constexpr int kBytes = 2;
+    static constexpr int row(int d) { return 2 * d; }
+    static constexpr int scales(int) { return 0; }
+};
+struct E4M3 {
+    static constexpr int kBytes = 1;
+    static constexpr int row(int d) { return d; }
+    static constexpr int scales(int) { return 1; }
+};
+struct E2M1 {
+    static constexpr int kBytes = 0, kBlock = 32;      // values that share an exponent byte
+    static constexpr int row(int d) { return d / 2; }
+    static constexpr int scales(int d) { return d / kBlock; }
+};
 
 __device__ inline float bf16_up(uint32_t bits) { return __uint_as_float(bits << 16); }
 // two floats to bfloat16, round to nearest even, the first in the low half
@@ -64,6 +83,33 @@ __device__ inline uint32_t codes2_bf16(uint32_t w, float scale, int high) {
 __device__ inline uint4 codes8_bf16(uint32_t w0, uint32_t w1, float scale) {
     return make_uint4(codes2_bf16(w0, scale, 0), codes2_bf16(w0, scale, 1), codes2_bf16(w1, scale, 0),
                       codes2_bf16(w1, scale, 1));
+}
+
+// 4 bits: codes 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign, the earlier value in a byte's low half.  The conversions take the
+// scale as an exponent byte at its place in a float: 0 is 2^-127, and 255 makes NaN of any code.  Down they round to
+// nearest even and keep a zero's sign; up they are exact but where the type itself ends.
+// The exponent byte of a block whose largest magnitude has the bits `top`: the smallest E in 2..252 that brings it to at
+// most 6 = 1.5 * 2^2 (past 252 the codes stay at 6, so that what is finite stays finite; from 2 on nothing that is stored
+// is subnormal); 255 for one that holds an infinity or NaN; 127 for zeros.
+__device__ inline uint32_t block_exponent(uint32_t top) {
+    const int E = int(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u ? 1 : 0);
+    return top >= 0x7f800000u ? 255u : top == 0 ? 127u : uint32_t(E < 2 ? 2 : E > 252 ? 252 : E);
+}
+// the codes of byte i of w
+template <int I>
+__device__ inline uint32_t pair_bf16(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, I));
+}
+template <int I>
+__device__ inline void pair_f32(uint32_t w, float scale, float &x, float &y) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const f2 r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, I);
+    x = r[0];
+    y = r[1];
+}
+// eight codes
+__device__ inline uint4 word_bf16(uint32_t w, float scale) {
+    return make_uint4(pair_bf16<0>(w, scale), pair_bf16<1>(w, scale), pair_bf16<2>(w, scale), pair_bf16<3>(w, scale));
 }
 
 __device__ inline void flag(const PageTables &t) {

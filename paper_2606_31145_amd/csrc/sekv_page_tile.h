@@ -56,8 +56,9 @@ __device__ inline float across16(float x) {
 __device__ inline uint32_t odd2(uint32_t w) { return uint32_t((w & 0x7f80u) == 0x7f80u) | uint32_t((w & 0x7f800000u) == 0x7f800000u); }
 __device__ inline uint32_t odd(const uint4 &v) { return odd2(v.x) | odd2(v.y) | odd2(v.z) | odd2(v.w); }
 __device__ inline bool odd(float x) { return !(fabsf(x) <= 3.402823466e38f); }
-// The first exponent byte whose rows may decode to infinities: 256 * 2^120 is past float and bfloat16.
-constexpr uint32_t kOverExponent = 247;
+// The first exponent byte whose rows may decode to infinities: 256 * 2^120 is past float and bfloat16, and so is
+// 6 * 2^126, which is not stored but may lie in a page of somebody else's.
+constexpr uint32_t kOverExponent = 247, kOverExponent4 = 253;
 // Is one of four e4m3 codes a NaN.
 __device__ inline uint32_t nan4(uint32_t w) {
     const uint32_t x = ~w & 0x7f7f7f7fu;               // a zero byte: NaN
@@ -307,8 +308,10 @@ __device__ inline void put(const PageAttendArgs &a, const Item &it, int chunk, i
 template <class T, class P, int D>
 struct Keys16 {
     static constexpr int kBlocks = T::kBytes == 2 ? 2 : 1, kKeys = 16 * kBlocks;
-    static constexpr int KW = D * P::kBytes / 16, VW = D * P::kBytes / 64;    // words a lane
-    uint32_t k[kBlocks][KW], v[kBlocks][4][VW], ks[kBlocks], vs[kBlocks];
+    static constexpr int kRow = P::row(D);
+    static constexpr int KW = kRow / 16, VW = kRow >= 64 ? kRow / 64 : 1;     // words a lane
+    static constexpr int SW = P::kBytes == 0 ? P::scales(D) : 1;              // words of the exponent bytes of four rows
+    uint32_t k[kBlocks][KW], v[kBlocks][4][VW], ks[kBlocks], vs[kBlocks][SW];
 
     __device__ static size_t base(int row) { return row >= 0 ? row : 0; }     // any row: its keys are masked
     __device__ void load_keys(const PageAttendArgs &a, const int (&row)[kBlocks], int lane) {
@@ -316,14 +319,19 @@ struct Keys16 {
 #pragma unroll
         for (int j = 0; j < kBlocks; ++j) {
             const size_t r0 = base(row[j]);
-            const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * (D * P::kBytes);
+            const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * kRow;
+            if constexpr (KW == 2) {
+                const uint2 w = *reinterpret_cast<const uint2 *>(kp + m * kRow + 8 * g);
+                k[j][0] = w.x; k[j][1] = w.y;
+            }
 #pragma unroll
             for (int i = 0; i < KW / 4; ++i) {
                 const int off = P::kBytes == 4 ? 256 * (i >> 2) + 64 * g + 16 * (i & 3) : 64 * i + 16 * g;
-                const uint4 w = *reinterpret_cast<const uint4 *>(kp + m * (D * P::kBytes) + off);
+                const uint4 w = *reinterpret_cast<const uint4 *>(kp + m * kRow + off);
                 k[j][4 * i] = w.x; k[j][4 * i + 1] = w.y; k[j][4 * i + 2] = w.z; k[j][4 * i + 3] = w.w;
             }
             if constexpr (P::kBytes == 1) ks[j] = a.k_scale[r0 + m];
+            if constexpr (P::kBytes == 0) ks[j] = a.k_scale[(r0 + m) * P::scales(D) + g * P::scales(D) / 4];
         }
     }
     __device__ void load_values(const PageAttendArgs &a, const int (&row)[kBlocks], int lane) {
@@ -331,11 +339,13 @@ struct Keys16 {
 #pragma unroll
         for (int j = 0; j < kBlocks; ++j) {
             const size_t r0 = base(row[j]);
-            const unsigned char *vp = static_cast<const unsigned char *>(a.v) + r0 * (D * P::kBytes);
+            const unsigned char *vp = static_cast<const unsigned char *>(a.v) + r0 * kRow;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const unsigned char *p = vp + (4 * g + i) * (D * P::kBytes) + m * (VW * 4);
-                if constexpr (VW % 4 == 0) {
+                const unsigned char *p = vp + (4 * g + i) * kRow + m * (kRow / 16);
+                if constexpr (kRow == 32) {
+                    v[j][i][0] = *reinterpret_cast<const uint16_t *>(p);
+                } else if constexpr (VW % 4 == 0) {
 #pragma unroll
                     for (int u = 0; u < VW / 4; ++u) {
                         const uint4 w = reinterpret_cast<const uint4 *>(p)[u];
@@ -348,8 +358,30 @@ struct Keys16 {
                     v[j][i][0] = *reinterpret_cast<const uint32_t *>(p);
                 }
             }
-            if constexpr (P::kBytes == 1) vs[j] = *reinterpret_cast<const uint32_t *>(a.v_scale + r0 + 4 * g);
+            if constexpr (P::kBytes == 1) vs[j][0] = *reinterpret_cast<const uint32_t *>(a.v_scale + r0 + 4 * g);
+            if constexpr (P::kBytes == 0) {
+                const uint32_t *s = reinterpret_cast<const uint32_t *>(a.v_scale + (r0 + 4 * g) * SW);
+                if constexpr (SW == 4) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(s);
+                    vs[j][0] = w.x; vs[j][1] = w.y; vs[j][2] = w.z; vs[j][3] = w.w;
+                } else {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(s);
+                    vs[j][0] = w.x; vs[j][1] = w.y;
+                }
+            }
         }
+    }
+    // Exponent byte of the values that the lane holds of row 4 g + i of block j; that of a row that counts as zeros.
+    __device__ static int shift(int i, int lane) {
+        const int m = lane & 15;
+        return P::kBytes == 1 ? 8 * i : SW == 4 ? 8 * (m >> 2) : 16 * (i & 1) + 8 * (m >> 3);
+    }
+    __device__ uint32_t scale(int j, int i, int lane) const {
+        return vs[j][P::kBytes == 1 ? 0 : SW == 4 ? i : i >> 1] >> shift(i, lane) & 255u;
+    }
+    __device__ void drop_scale(int j, int i, int lane) {
+        uint32_t &w = vs[j][P::kBytes == 1 ? 0 : SW == 4 ? i : i >> 1];
+        w = (w & ~(255u << shift(i, lane))) | 127u << shift(i, lane);
     }
 };
 
@@ -383,8 +415,9 @@ struct Rows16 {
 #pragma unroll
             for (int i = 0; i < QW / 4; ++i) {
                 // the dims of product i: as Keys16 lays out its pieces
-                const int dim = !kBf ? 64 * (i >> 2) + 16 * gq + 4 * (i & 3)
+                const int whole = !kBf ? 64 * (i >> 2) + 16 * gq + 4 * (i & 3)
                               : P::kBytes == 2 ? 32 * i + 8 * gq : 64 * (i >> 1) + 16 * gq + 8 * (i & 1);
+                const int dim = P::kBytes == 0 ? D / 4 * gq + (kBf ? 8 : 4) * i : whole;
                 const uint4 w = *reinterpret_cast<const uint4 *>(src + dim);
                 q[nb][4 * i] = w.x; q[nb][4 * i + 1] = w.y; q[nb][4 * i + 2] = w.z; q[nb][4 * i + 3] = w.w;
             }
@@ -406,6 +439,8 @@ struct Rows16 {
     __device__ static uint4 k_frag(const Tile &t, int j, int s) {             // bfloat16: product s
         if constexpr (P::kBytes == 2) {
             return make_uint4(t.k[j][4 * s], t.k[j][4 * s + 1], t.k[j][4 * s + 2], t.k[j][4 * s + 3]);
+        } else if constexpr (P::kBytes == 0) {
+            return word_bf16(t.k[j][s], pow2_of(t.ks[j]));
         } else {
             return codes8_bf16(t.k[j][2 * s], t.k[j][2 * s + 1], pow2_of(t.ks[j]));
         }
@@ -440,6 +475,10 @@ struct Rows16 {
                     if constexpr (P::kBytes == 4) {
 #pragma unroll
                         for (int u = 0; u < 4; ++u) kf[u] = __uint_as_float(t.k[j][4 * i + u]);
+                    } else if constexpr (P::kBytes == 0) {
+                        const uint32_t w = t.k[j][i >> 1] >> (16 * (i & 1));
+                        pair_f32<0>(w, pow2_of(t.ks[j]), kf[0], kf[1]);
+                        pair_f32<1>(w, pow2_of(t.ks[j]), kf[2], kf[3]);
                     } else {
                         codes4_up(t.k[j][i], pow2_of(t.ks[j]), kf);
                     }
@@ -529,15 +568,16 @@ struct Rows16 {
                     const uint32_t keep = (valid >> j & 1) && key >= lo_any && key <= hi_any ? 0xffffffffu : 0u;
                     uint32_t wrong = 0;
                     // the exponent byte as well: one of 255 makes no number of any code
-                    if constexpr (P::kBytes == 1) {
-                        t.vs[j] = keep ? t.vs[j] : (t.vs[j] & ~(255u << (8 * i))) | 127u << (8 * i);
-                        wrong = uint32_t((t.vs[j] >> (8 * i) & 255u) >= kOverExponent);
+                    if constexpr (P::kBytes <= 1) {
+                        if (!keep) t.drop_scale(j, i, lane);
+                        wrong = uint32_t(t.scale(j, i, lane) >= (P::kBytes == 1 ? kOverExponent : kOverExponent4));
                     }
 #pragma unroll
                     for (int w = 0; w < Tile::VW; ++w) {
                         t.v[j][i][w] &= keep;
-                        wrong |= P::kBytes == 1 ? nan4(t.v[j][i][w]) : P::kBytes == 2 ? odd2(t.v[j][i][w])
-                                                                              : uint32_t(odd(__uint_as_float(t.v[j][i][w])));
+                        if constexpr (P::kBytes == 1) wrong |= nan4(t.v[j][i][w]);
+                        if constexpr (P::kBytes == 2) wrong |= odd2(t.v[j][i][w]);
+                        if constexpr (P::kBytes == 4) wrong |= uint32_t(odd(__uint_as_float(t.v[j][i][w])));
                     }
                     *bad |= wrong != 0;
                 }
@@ -556,7 +596,8 @@ struct Rows16 {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (P::kBytes == 2) x[j][i] = t.v[j][i][w];
-                        else x[j][i] = codes2_bf16(t.v[j][i][w / 2], pow2_of(t.vs[j] >> (8 * i) & 255u), w & 1);
+                        else if constexpr (P::kBytes == 1) x[j][i] = codes2_bf16(t.v[j][i][w / 2], pow2_of(t.scale(j, i, lane)), w & 1);
+                        else x[j][i] = pair_bf16<0>(t.v[j][i][0] >> (8 * w), pow2_of(t.scale(j, i, lane)));
                     }
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -575,11 +616,15 @@ struct Rows16 {
                 if constexpr (P::kBytes == 4) {
 #pragma unroll
                     for (int e = 0; e < VE; ++e) vf[e] = __uint_as_float(t.v[0][i][e]);
+                } else if constexpr (P::kBytes == 0) {
+#pragma unroll
+                    for (int w = 0; w < VE / 2; ++w)
+                        pair_f32<0>(t.v[0][i][0] >> (8 * w), pow2_of(t.scale(0, i, lane)), vf[2 * w], vf[2 * w + 1]);
                 } else {
 #pragma unroll
                     for (int w = 0; w < VE / 4; ++w) {
                         float x[4];
-                        codes4_up(t.v[0][i][w], pow2_of(t.vs[0] >> (8 * i) & 255u), x);
+                        codes4_up(t.v[0][i][w], pow2_of(t.scale(0, i, lane)), x);
 #pragma unroll
                         for (int u = 0; u < 4; ++u) vf[4 * w + u] = x[u];
                     }
@@ -596,7 +641,7 @@ struct Rows16 {
     // A group's keys and values are asked for as soon as the registers of an earlier one are free, kAhead groups
     // ahead; its row blocks one group before that.  Two groups where they fit: 32 ragged sequences in bfloat16 462 us
     // against 469 with one, 4 of 131072 in 8 bits 188.6 against 191.2, 13 of float and head_dim 64 577 against 599.
-    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW), kHeld = NB * (D / 4 + QW);
+    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 1 + Tile::SW : 0)), kHeld = NB * (D / 4 + QW);
     static constexpr int kAhead = 2 * kTileWords + kHeld <= 176 ? 2 : 1;      // of 256 registers
     __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int step, bool *bad, int lane) {
         if (pos >= it.end) return;
@@ -656,7 +701,12 @@ template <class T, class P, int D>
 __device__ inline void plain_rows(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave) {
     auto element = [](const void *pool, const uint8_t *scale, int row, int i) {
         const size_t at = size_t(row) * D + i;
-        if constexpr (P::kBytes == 4) return static_cast<const float *>(pool)[at];
+        if constexpr (P::kBytes == 0) {
+            float x, y;
+            pair_f32<0>(uint32_t(static_cast<const uint8_t *>(pool)[at >> 1]) >> (4 * (i & 1)),
+                        pow2_of(scale[at / P::kBlock]), x, y);
+            return x;
+        } else if constexpr (P::kBytes == 4) return static_cast<const float *>(pool)[at];
         else if constexpr (P::kBytes == 2) return bf16_up(static_cast<const uint16_t *>(pool)[at]);
         else {
             float x[4];

@@ -50,7 +50,7 @@ template <int D> struct Swizzle {
 };
 
 // A wave's 16 rows of 8-bit keys and values on their way from a page into LDS, where they are bfloat16.
-template <int D>
+template <class P, int D>
 struct Stage {
     static constexpr int N = D / 64;                   // 16-byte pieces a lane, keys or values
     static constexpr int PC = D / 16;                  // pieces a row
@@ -97,6 +97,42 @@ struct Stage {
             *reinterpret_cast<uint4 *>(kr + (((2 * c + 1) ^ Z::key(row)) << 4)) = codes8_bf16(k[i].z, k[i].w, fk);
             *reinterpret_cast<uint4 *>(vr + (((2 * c) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].x, v[i].y, fv);
             *reinterpret_cast<uint4 *>(vr + (((2 * c + 1) ^ Z::value(row)) << 4)) = codes8_bf16(v[i].z, v[i].w, fv);
+        }
+    }
+};
+
+// The same in 4 bits: a lane holds a quarter of a row, which at head_dim 128 is a block with its own exponent byte.
+template <int D>
+struct Stage<E2M1, D> {
+    static constexpr int W = D / 32;                   // words a lane, of eight codes each
+    typedef uint32_t wv __attribute__((ext_vector_type(W)));
+    wv k, v;
+    uint32_t ks, vs;
+
+    __device__ void load(const PageAttendArgs &a, int row0, int lane) {
+        const size_t r0 = row0 >= 0 ? row0 : 0;        // any row: its keys are masked
+        k = reinterpret_cast<const wv *>(static_cast<const unsigned char *>(a.k) + r0 * E2M1::row(D))[lane];
+        v = reinterpret_cast<const wv *>(static_cast<const unsigned char *>(a.v) + r0 * E2M1::row(D))[lane];
+        ks = a.k_scale[r0 * E2M1::scales(D) + lane * E2M1::scales(D) / 4];
+        vs = a.v_scale[r0 * E2M1::scales(D) + lane * E2M1::scales(D) / 4];
+    }
+    // as above
+    __device__ bool mend(int row0, int from, int end, int lane) {
+        const int row = row0 + lane / 4;
+        const uint32_t keep = row >= from && row < end ? ~0u : 0u;
+        v &= keep;
+        vs = keep ? vs : 127u;
+        return vs >= kOverExponent4;
+    }
+    __device__ void store(unsigned char *kt, unsigned char *vt, int row0, int lane) const {
+        using Z = Swizzle<D>;
+        const int row = row0 + lane / 4, c = lane % 4 * W;
+        unsigned char *kr = kt + row * (D * 2), *vr = vt + row * (D * 2);
+        const float fk = pow2_of(ks), fv = pow2_of(vs);
+#pragma unroll
+        for (int u = 0; u < W; ++u) {
+            *reinterpret_cast<uint4 *>(kr + (((c + u) ^ Z::key(row)) << 4)) = word_bf16(k[u], fk);
+            *reinterpret_cast<uint4 *>(vr + (((c + u) ^ Z::value(row)) << 4)) = word_bf16(v[u], fv);
         }
     }
 };

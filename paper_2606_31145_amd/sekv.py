@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libsekv_trace.so" if os.environ.get("SEKV_LIB") =
                         else "libsekv.so")
 
 SEKV_OK, SEKV_ERR_INVALID_ARG, SEKV_ERR_UNSUPPORTED, SEKV_ERR_WORKSPACE, SEKV_ERR_HIP = range(5)
-SEKV_F32, SEKV_BF16, SEKV_E4M3 = 0, 1, 2
+SEKV_F32, SEKV_BF16, SEKV_E4M3, SEKV_E2M1 = 0, 1, 2, 3
 SEKV_ZOOM_DEFAULT, SEKV_ZOOM_FACTORED = 0, 1
 SEKV_TIER_GATHER, SEKV_TIER_MEMCPY = 0, 1
 TIER_MODES = {"gather": SEKV_TIER_GATHER, "memcpy": SEKV_TIER_MEMCPY}
@@ -698,12 +698,14 @@ def build_layer(bd: BuildDims, keys, values, surprisal, n_tokens, omega, ws: Wor
 # paged token store
 # ---------------------------------------------------------------------------
 
+_PAGE_CODES = dict(DTYPE_CODES, e4m3=SEKV_E4M3, e2m1=SEKV_E2M1)
+
+
 def make_page_dims(*, batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, dtype,
                    page_dtype=None, window=0, softmax_scale) -> PageDims:
-    """dtype "f32" or "bf16"; page_dtype the same (default) or "e4m3"."""
+    """dtype "f32" or "bf16"; page_dtype the same (default), "e4m3" or "e2m1"."""
     dt = DTYPE_CODES[dtype] if isinstance(dtype, str) else int(dtype)
-    pt = dt if page_dtype is None else SEKV_E4M3 if page_dtype == "e4m3" else \
-        DTYPE_CODES[page_dtype] if isinstance(page_dtype, str) else int(page_dtype)
+    pt = dt if page_dtype is None else _PAGE_CODES[page_dtype] if isinstance(page_dtype, str) else int(page_dtype)
     return PageDims(batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, dt, pt, int(window),
                     (ctypes.c_int32 * 2)(0, 0), float(softmax_scale))
 
@@ -720,13 +722,23 @@ def page_workspace_size(pd: PageDims, new_tokens: int) -> int:
     return n
 
 
-_PAGE_STORAGE = {SEKV_F32: torch.float32, SEKV_BF16: torch.bfloat16, SEKV_E4M3: torch.float8_e4m3fn}
+_PAGE_STORAGE = {SEKV_F32: torch.float32, SEKV_BF16: torch.bfloat16, SEKV_E4M3: torch.float8_e4m3fn,
+                 SEKV_E2M1: torch.uint8}
+
+
+def _page_shapes(pd: PageDims):
+    """(shape of a pool, shape of its exponents where it has them)"""
+    rows = (pd.n_pages, pd.n_kv_heads, pd.page_size)
+    if pd.page_dtype == SEKV_E2M1:
+        return rows + (pd.head_dim // 2,), rows + (pd.head_dim // 32,)
+    return rows + (pd.head_dim,), rows
 
 
 class PageCache:
     """Device tensors of one layer's pages, laid out as sekv_pages describes: pools
     [n_pages][Hkv][page_size][d] (float8_e4m3fn with uint8 exponents [n_pages][Hkv][page_size],
-    or the tokens' own type without), page table int32 [B][max_pages], seq_len int32 [B]."""
+    or the tokens' own type without; in 4 bits uint8 [n_pages][Hkv][page_size][d / 2] with uint8
+    exponents [n_pages][Hkv][page_size][d / 32]), page table int32 [B][max_pages], seq_len int32 [B]."""
 
     def __init__(self, k_pages, v_pages, page_table, seq_len, k_scale=None, v_scale=None):
         self.k_pages, self.v_pages = k_pages, v_pages
@@ -741,11 +753,11 @@ class PageCache:
     def empty(cls, pd: PageDims, page_table, seq_len, device="cuda"):
         """Pools of zeros for pd."""
         check_page_dims(pd)
-        shape = (pd.n_pages, pd.n_kv_heads, pd.page_size, pd.head_dim)
+        shape, scales = _page_shapes(pd)
         k, v = (torch.zeros(shape, dtype=_PAGE_STORAGE[pd.page_dtype], device=device) for _ in "kv")
-        if pd.page_dtype != SEKV_E4M3:
+        if pd.page_dtype not in (SEKV_E4M3, SEKV_E2M1):
             return cls(k, v, page_table, seq_len)
-        ks, vs = (torch.full(shape[:-1], 127, dtype=torch.uint8, device=device) for _ in "kv")
+        ks, vs = (torch.full(scales, 127, dtype=torch.uint8, device=device) for _ in "kv")
         return cls(k, v, page_table, seq_len, ks, vs)
 
     def _tensors(self):
@@ -758,16 +770,15 @@ class PageCache:
         seen = (bytes(pd), *[None if x is None else x.data_ptr() for x in self._tensors()])
         if seen == self._seen:
             return self._struct
-        rows = (pd.n_pages, pd.n_kv_heads, pd.page_size)
+        pool, scales = _page_shapes(pd)
         want = _PAGE_STORAGE[pd.page_dtype] if pd.page_dtype in _PAGE_STORAGE else None
         dev = self.k_pages.device
-        for name, x, dt, shape in (("k_pages", self.k_pages, want, rows + (pd.head_dim,)),
-                                   ("v_pages", self.v_pages, want, rows + (pd.head_dim,)),
-                                   ("k_scale", self.k_scale, torch.uint8, rows),
-                                   ("v_scale", self.v_scale, torch.uint8, rows),
+        for name, x, dt, shape in (("k_pages", self.k_pages, want, pool), ("v_pages", self.v_pages, want, pool),
+                                   ("k_scale", self.k_scale, torch.uint8, scales),
+                                   ("v_scale", self.v_scale, torch.uint8, scales),
                                    ("page_table", self.page_table, torch.int32, (pd.batch, pd.max_pages)),
                                    ("seq_len", self.seq_len, torch.int32, (pd.batch,))):
-            if x is None and dt is torch.uint8:
+            if x is None and name.endswith("scale"):
                 continue
             _expect(x, name, dt, shape, dev)
         object.__setattr__(self, "_struct", PagesStruct(*[_ptr(x) for x in self._tensors()]))
