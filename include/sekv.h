@@ -416,6 +416,60 @@ SEKV_API sekv_status sekv_page_append(const sekv_page_dims *dims, const sekv_pag
                                       const int32_t *tok_start, int32_t n_tokens, void *ws, size_t ws_bytes,
                                       hipStream_t stream);
 
+/* Rotary positions (Su et al. 2021): pair i of a token at position p turns by the angle a = p freq[i],
+ *   x' = scale (x cos a - y sin a),  y' = scale (y cos a + x sin a),
+ * over the first rot_dim values of a head; those behind stay as they are.  Pairs are (i, i + rot_dim / 2) in
+ * the half layout, (2 i, 2 i + 1) in the interleaved one.  Angles, their cosines and the products are formed
+ * in double and rounded to float, and that to the rows' type. */
+typedef enum { SEKV_ROTARY_HALF = 0, SEKV_ROTARY_INTERLEAVED = 1 } sekv_rotary_layout;
+typedef struct {
+    int32_t rot_dim;        /* a multiple of 16, at most head_dim                          */
+    int32_t layout;         /* sekv_rotary_layout                                          */
+    const double *freq;     /* device [rot_dim / 2]: radians a position                    */
+    double scale;           /* of the turned values, in [1e-30, 1e30]; 1 unless stretched  */
+} sekv_rotary;
+
+/* Frequencies for a longer context than the one trained on.  With f_i = base^(-2 i / rot_dim):
+ *   PLAIN   f_i
+ *   LINEAR  f_i / factor (Chen et al. 2023)
+ *   BASE    f_i of the base base * factor^(rot_dim / (rot_dim - 2)): the first pair stays, the last one's
+ *           frequency is divided by factor
+ *   BANDS   pairs that turn more than `high` times over `trained` positions stay, those that turn fewer than
+ *           `low` times are divided by factor, those between are mixed linearly in their turns
+ *   RAMP    the same, but mixed linearly in the pair's index, and scale = 0.1 ln(factor) + 1 (Peng et al. 2023)
+ * scale is 1 for the others.  Host memory: freq [rot_dim / 2], scale [1]. */
+typedef enum {
+    SEKV_ROTARY_PLAIN = 0, SEKV_ROTARY_LINEAR = 1, SEKV_ROTARY_BASE = 2, SEKV_ROTARY_BANDS = 3, SEKV_ROTARY_RAMP = 4
+} sekv_rotary_scaling;
+typedef struct {
+    int32_t rot_dim;        /* even, 2..4096                                               */
+    int32_t scaling;        /* sekv_rotary_scaling                                         */
+    double base;            /* > 1                                                         */
+    double factor;          /* >= 1 (not PLAIN)                                            */
+    double trained;         /* > 0 positions (BANDS, RAMP)                                 */
+    double low, high;       /* 0 < low < high turns (BANDS, RAMP)                          */
+} sekv_rotary_spec;
+SEKV_API sekv_status sekv_rotary_frequencies(const sekv_rotary_spec *spec, double *freq, double *scale);
+
+/* Turn rows by themselves: x and y [n_tokens][n_heads][head_dim] in dtype (F32 or BF16), consecutive tokens
+ * x_stride and y_stride elements apart (at least n_heads * head_dim; 16-byte multiples).  y may be x itself;
+ * other rows of the two do not overlap.  positions: device int32 [n_tokens], of any sign.  transpose = 1 turns
+ * the other way, with the same scale: the gradient with respect to x of a call with transpose = 0.  No workspace. */
+SEKV_API sekv_status sekv_rotate(const sekv_rotary *rotary, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                                 int32_t dtype, const void *x, int64_t x_stride, void *y, int64_t y_stride,
+                                 const int32_t *positions, int32_t transpose, hipStream_t stream);
+
+/* sekv_page_append of keys that are turned on the way: from the float that the rotation gives they are stored
+ * as unturned ones are.  Values are stored as they are.  q and q_out [n_tokens][Hq][d] (NULL together: no
+ * queries): the queries turned in the same launch, for every token that belongs to a sequence; q_out may be q
+ * itself and does not overlap anything else.  positions: device int32 [n_tokens], or NULL for each token's
+ * position in its sequence; where it is stored does not depend on it. */
+SEKV_API sekv_status sekv_page_append_rotary(const sekv_page_dims *dims, const sekv_pages *pages,
+                                             const sekv_rotary *rotary, const void *q, int64_t q_stride, void *q_out,
+                                             int64_t q_out_stride, const void *k, const void *v, int64_t k_stride,
+                                             int64_t v_stride, const int32_t *positions, const int32_t *tok_start,
+                                             int32_t n_tokens, void *ws, size_t ws_bytes, hipStream_t stream);
+
 /* Read rows 0 .. min(seq_len[b], max_tokens) - 1 of every sequence into keys and values
  * [B][Hkv][max_tokens][d] in dims.dtype (the layout of sekv_build_cache); rows behind, and
  * rows whose page is outside the pool, are left as they are. */

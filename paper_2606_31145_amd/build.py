@@ -58,7 +58,8 @@ def _jobs(bdir, trace):
         jobs.append(([HIPCC, *COMMON, f"--offload-arch={ARCH}", *DEVICE_FLAGS, *tflag,
                       f"-DSEKV_T={t}", f"-DSEKV_D={d}", "-c",
                       os.path.join(CSRC, "sekv_step_inst.hip"), "-o", obj], obj))
-    for src in ("sekv_kernels.hip", "sekv_tier.hip", "sekv_noalloc.hip", "sekv_gate.hip", "sekv_page.hip"):
+    for src in ("sekv_kernels.hip", "sekv_tier.hip", "sekv_noalloc.hip", "sekv_gate.hip", "sekv_page.hip",
+                "sekv_rotary.hip"):
         obj = os.path.join(bdir, src.replace(".hip", ".o"))
         jobs.append(([HIPCC, *COMMON, f"--offload-arch={ARCH}", *DEVICE_FLAGS, "-c",
                       os.path.join(CSRC, src), "-o", obj], obj))

@@ -355,6 +355,61 @@ sekv_status check_pages(const sekv_page_dims *d, const sekv_pages *p) {
     return SEKV_OK;
 }
 
+// ---- rotary positions ------------------------------------------------------------------
+
+sekv_status check_rotary(const sekv_rotary *r, int head_dim) {
+    if (!r) return fail(SEKV_ERR_INVALID_ARG, "rotary is NULL");
+    if (r->rot_dim < 16 || r->rot_dim > head_dim || r->rot_dim % 16)
+        return fail(SEKV_ERR_UNSUPPORTED, "rot_dim %d: a multiple of 16 in [16, %d]", r->rot_dim, head_dim);
+    if (r->layout != SEKV_ROTARY_HALF && r->layout != SEKV_ROTARY_INTERLEAVED)
+        return fail(SEKV_ERR_INVALID_ARG, "rotary layout %d", r->layout);
+    if (!r->freq || misaligned(r->freq, 8)) return fail(SEKV_ERR_INVALID_ARG, "rotary.freq is NULL or not 8-byte aligned");
+    if (!(r->scale > 0.0) || !std::isfinite(r->scale))
+        return fail(SEKV_ERR_INVALID_ARG, "rotary.scale must be finite and > 0");
+    if (r->scale < 1e-30 || r->scale > 1e30) return fail(SEKV_ERR_UNSUPPORTED, "rotary.scale %g outside [1e-30, 1e30]", r->scale);
+    return SEKV_OK;
+}
+
+sekv_status rotary_frequencies(const sekv_rotary_spec *p, double *freq, double *scale) {
+    if (!p || !freq || !scale) return fail(SEKV_ERR_INVALID_ARG, "rotary spec, freq or scale is NULL");
+    if (p->rot_dim < 2 || p->rot_dim > 4096 || p->rot_dim % 2)
+        return fail(SEKV_ERR_UNSUPPORTED, "rot_dim %d: even, in [2, 4096]", p->rot_dim);
+    if (p->scaling < SEKV_ROTARY_PLAIN || p->scaling > SEKV_ROTARY_RAMP)
+        return fail(SEKV_ERR_INVALID_ARG, "rotary scaling %d", p->scaling);
+    if (!(p->base > 1.0) || !std::isfinite(p->base)) return fail(SEKV_ERR_INVALID_ARG, "base must be finite and > 1");
+    const bool plain = p->scaling == SEKV_ROTARY_PLAIN;
+    const bool lengths = p->scaling == SEKV_ROTARY_BANDS || p->scaling == SEKV_ROTARY_RAMP;
+    if (!plain && (!(p->factor >= 1.0) || !std::isfinite(p->factor)))
+        return fail(SEKV_ERR_INVALID_ARG, "factor must be finite and >= 1");
+    if (lengths && (!(p->trained > 0.0) || !std::isfinite(p->trained) || !(p->low > 0.0) || !(p->high > p->low) ||
+                    !std::isfinite(p->high)))
+        return fail(SEKV_ERR_INVALID_ARG, "trained > 0 and 0 < low < high are needed");
+    const int n = p->rot_dim / 2;
+    const double two_pi = 6.283185307179586476925, R = p->rot_dim;
+    if (p->scaling == SEKV_ROTARY_BASE && p->rot_dim == 2)
+        return fail(SEKV_ERR_UNSUPPORTED, "a stretched base needs two pairs at least");
+    const double base = p->scaling == SEKV_ROTARY_BASE ? p->base * std::pow(p->factor, R / (R - 2.0)) : p->base;
+    // the pair, as a real number, that turns so many times over the trained positions
+    auto pair_of = [&](double turns) { return R * std::log(p->trained / (turns * two_pi)) / (2.0 * std::log(p->base)); };
+    double from = 0.0, to = 0.0;
+    if (p->scaling == SEKV_ROTARY_RAMP) {
+        from = std::fmax(std::floor(pair_of(p->high)), 0.0);
+        to = std::fmin(std::ceil(pair_of(p->low)), R - 1.0);
+        if (to <= from) to = from + 1e-3;
+    }
+    for (int i = 0; i < n; ++i) {
+        double f = std::pow(base, -2.0 * i / R);
+        double keep = 1.0;                                   // of the frequency as it was; the rest divided by factor
+        if (p->scaling == SEKV_ROTARY_LINEAR) keep = 0.0;
+        if (p->scaling == SEKV_ROTARY_BANDS) keep = (p->trained * f / two_pi - p->low) / (p->high - p->low);
+        if (p->scaling == SEKV_ROTARY_RAMP) keep = 1.0 - (i - from) / (to - from);
+        keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+        freq[i] = keep == 1.0 ? f : keep * f + (1.0 - keep) * (f / p->factor);
+    }
+    *scale = p->scaling == SEKV_ROTARY_RAMP ? 0.1 * std::log(p->factor) + 1.0 : 1.0;
+    return SEKV_OK;
+}
+
 // ---- prefill-side builder: dims check and the factor arena's layout -----------------
 
 sekv_status check_build_dims(const sekv_build_dims *d) {

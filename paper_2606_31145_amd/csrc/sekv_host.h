@@ -90,6 +90,8 @@ class WsTracker {
 sekv_status check_page_dims(const sekv_page_dims *d);
 // Pointer checks of a page store (null, alignment, scales present just when they are used).
 sekv_status check_pages(const sekv_page_dims *d, const sekv_pages *p);
+sekv_status check_rotary(const sekv_rotary *r, int head_dim);
+sekv_status rotary_frequencies(const sekv_rotary_spec *spec, double *freq, double *scale);
 
 // ---- prefill-side builder ------------------------------------------------------------
 sekv_status check_build_dims(const sekv_build_dims *d);

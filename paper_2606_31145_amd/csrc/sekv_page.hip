@@ -9,7 +9,7 @@
 
 #include <type_traits>
 
-#include "sekv_page_row.h"
+#include "sekv_page_store.h"
 
 namespace sekv {
 
@@ -33,142 +33,6 @@ using namespace page;
 
 constexpr int kThreads = 256;
 constexpr int64_t kMaxBlocks = 1 << 21;   // a launch stays below 2^32 threads
-typedef uint32_t u4v __attribute__((ext_vector_type(4)));
-
-// The largest of L lanes' words, in each of them (L = 4, 8, 16, 32; a group of lanes starts at a multiple of L).
-template <int L>
-__device__ inline uint32_t lanes_max(uint32_t x) {
-    auto with = [&](uint32_t y) { x = x > y ? x : y; };
-    with(__builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true));       // quad_perm: lane ^ 1
-    with(__builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true));       // quad_perm: lane ^ 2
-    if constexpr (L >= 8) with(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));    // 7 - lane of 8
-    if constexpr (L >= 16) with(__builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));   // 15 - lane of 16
-    if constexpr (L >= 32) with(__shfl_xor(x, 16));
-    return x;
-}
-
-// 16 bytes of a row: as floats; the bits of the largest magnitude as a float's (an infinity's or NaN's if there
-// is one); four of its values as 8-bit codes, all of them as 4-bit codes, scaled by the power of two.
-template <class T> struct Piece;
-template <> struct Piece<F32> {
-    static constexpr int kN = 4;
-    static __device__ void up(const u4v &w, float (&x)[4]) {
-        x[0] = __uint_as_float(w[0]); x[1] = __uint_as_float(w[1]); x[2] = __uint_as_float(w[2]); x[3] = __uint_as_float(w[3]);
-    }
-    static __device__ uint32_t top(const u4v &w) {
-        const uint32_t a = w[0] & 0x7fffffffu, b = w[1] & 0x7fffffffu, c = w[2] & 0x7fffffffu, d = w[3] & 0x7fffffffu;
-        const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
-        return ab > cd ? ab : cd;
-    }
-    static __device__ uint32_t codes4(const u4v &w, float scale) {
-        const uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(w[0]), __uint_as_float(w[1]), scale, 0);
-        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(w[2]), __uint_as_float(w[3]), scale, 1);
-    }
-    static __device__ uint32_t codes(const u4v &w, int, float scale) {
-        typedef short s2v __attribute__((ext_vector_type(2)));
-        s2v r = {0, 0};
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __uint_as_float(w[0]), __uint_as_float(w[1]), scale, false);
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __uint_as_float(w[2]), __uint_as_float(w[3]), scale, true);
-        return __builtin_bit_cast(uint32_t, r);
-    }
-};
-template <> struct Piece<BF16> {
-    static constexpr int kN = 8;
-    static __device__ void up(const u4v &w, float (&x)[8]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = bf16_up(w[i] & 0xffffu);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
-    static __device__ uint32_t top(const u4v &w) {
-        typedef uint16_t h2v __attribute__((ext_vector_type(2)));
-        auto h = [&](int i) { return __builtin_bit_cast(h2v, w[i] & 0x7fff7fffu); };
-        const h2v m = __builtin_elementwise_max(__builtin_elementwise_max(h(0), h(1)), __builtin_elementwise_max(h(2), h(3)));
-        return uint32_t(m[0] > m[1] ? m[0] : m[1]) << 16;
-    }
-    static __device__ uint32_t codes4(const u4v &w, float scale) {
-        typedef __bf16 b2v __attribute__((ext_vector_type(2)));
-        const uint32_t a = w[0], b = w[1], c = w[2], d = w[3];   // a bit cast of w[k] itself takes element 0
-        uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(b2v, a), scale, 0);
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(b2v, b), scale, 1);
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(b2v, c), scale, 2);
-        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(b2v, d), scale, 3);
-    }
-    static __device__ uint32_t codes(const u4v &w, int i, float scale) {
-        typedef short s2v __attribute__((ext_vector_type(2)));
-        typedef __bf16 b2v __attribute__((ext_vector_type(2)));
-        s2v r = {0, 0};
-        const uint32_t lo = w[2 * i], hi = w[2 * i + 1];     // a bit cast of w[k] itself takes element 0
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(b2v, lo), scale, false);
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(b2v, hi), scale, true);
-        return __builtin_bit_cast(uint32_t, r);
-    }
-};
-
-// The place of new token `tok`: its sequence by a search in `start` (LDS), its row in the pool, or -1 (flagged).
-__device__ inline int place(const PageTables &t, const int32_t *start, int tok, int g, bool first_lane) {
-    if (tok >= start[t.B] || tok < start[0]) return -1;      // nobody's
-    int lo = 0, hi = t.B;                                    // the last b with start[b] <= tok
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= tok) lo = mid; else hi = mid;
-    }
-    const int64_t pos = int64_t(t.seq_len[lo]) - start[lo + 1] + tok;
-    int to = -1;
-    if (tok < start[lo + 1] && pos >= 0 && (pos >> t.page_shift) < t.max_pages) to = pool_row(t, lo, g, int(pos));
-    if (to < 0 && first_lane) flag(t);
-    return to;
-}
-
-template <class T, class P, int D>
-__device__ inline void store_row(const PageAppendArgs &a, int side, int to, const u4v &w, int lane) {
-    constexpr int N = Piece<T>::kN, L = D / N;
-    if constexpr (P::kBytes == T::kBytes) {
-        __builtin_nontemporal_store(w, reinterpret_cast<u4v *>(static_cast<unsigned char *>(a.pool[side]) + size_t(to) * (D * T::kBytes)) + lane);
-    } else if constexpr (P::kBytes == 0) {
-        constexpr int LB = P::kBlock / N;                    // lanes of a block
-        const uint32_t Ex = block_exponent(lanes_max<LB>(Piece<T>::top(w)));
-        const uint32_t c = Piece<T>::codes4(w, pow2_of(Ex));
-        unsigned char *dst = static_cast<unsigned char *>(a.pool[side]) + size_t(to) * P::row(D) + lane * (N / 2);
-        if constexpr (N == 8) __builtin_nontemporal_store(c, reinterpret_cast<uint32_t *>(dst));
-        else __builtin_nontemporal_store(uint16_t(c), reinterpret_cast<uint16_t *>(dst));
-        if (lane % LB == 0) a.scale[side][size_t(to) * P::scales(D) + lane / LB] = uint8_t(Ex);
-    } else {
-        uint32_t c[N / 4];
-        float m = __uint_as_float(lanes_max<L>(Piece<T>::top(w)));
-        uint32_t Ex = row_exponent(m);
-        if (m <= 3.402823466e38f && Ex > 8) {                // the row's lanes agree
-            const float scale = pow2_of(Ex);
-#pragma unroll
-            for (int i = 0; i < N / 4; ++i) c[i] = Piece<T>::codes(w, i, scale);
-        } else {
-            // infinities or NaN, which do not count for the scale, or values so small that they may be
-            // subnormal: element by element
-            float x[N];
-            Piece<T>::up(w, x);
-            m = 0.f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float y = fabsf(x[i]);
-                m = y <= 3.402823466e38f ? fmaxf(m, y) : m;
-            }
-            m = __uint_as_float(lanes_max<L>(__float_as_uint(m)));
-            Ex = row_exponent(m);
-            const float inv = pow2_of(254u - Ex);
-#pragma unroll
-            for (int i = 0; i < N / 4; ++i) {
-                const float y[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-                c[i] = codes4(y, inv);
-            }
-        }
-        unsigned char *dst = static_cast<unsigned char *>(a.pool[side]) + size_t(to) * D + lane * N;
-        typedef uint32_t u2v __attribute__((ext_vector_type(2)));
-        if constexpr (N == 8) __builtin_nontemporal_store((u2v{c[0], c[1]}), reinterpret_cast<u2v *>(dst));
-        else __builtin_nontemporal_store(c[0], reinterpret_cast<uint32_t *>(dst));
-        if (lane == 0) a.scale[side][to] = uint8_t(Ex);
-    }
-}
 
 // A block of consecutive new tokens of one head, heads side by side as they lie in a token: consecutive
 // tokens are consecutive rows of a page, so that what a workgroup writes, exponent bytes included, lies
@@ -200,10 +64,12 @@ __global__ void __launch_bounds__(kThreads) append_kernel(PageAppendArgs a) {
             __syncthreads();
             first = false;
         }
-        const int to = tok < t.n_tokens ? place(t, start, int(tok), g, lane == 0) : -1;
+        const int b = tok < t.n_tokens ? sequence_of(t, start, int(tok)) : -1;
+        const int to = b < 0 ? -1 : first_row(t, b, position_of(t, start, b, int(tok)));
+        if (b >= 0 && to < 0 && lane == 0) flag(t);
         if (to >= 0) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) store_row<T, P, D>(a, s, to, w[s], lane);
+            for (int s = 0; s < 2; ++s) store_row<Piece<T>, P, D>(a.pool[s], a.scale[s], to + (g << t.page_shift), Piece<T>{w[s]}, lane);
         }
     }
     if (blockIdx.x == 0) {                                   // offsets that cannot be

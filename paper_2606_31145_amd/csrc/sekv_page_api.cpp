@@ -39,14 +39,38 @@ sekv_status check_call(const sekv_page_dims *d, const sekv_pages *p, void *ws, s
 }
 
 // Consecutive tokens `stride` elements apart, each `heads` rows of d.
-sekv_status check_rows(const sekv_page_dims *d, const void *p, int64_t stride, int heads, const char *name) {
-    const int e = sekv::elem_bytes(d->dtype);
+sekv_status check_rows(int dtype, int head_dim, const void *p, int64_t stride, int heads, const char *name) {
+    const int e = sekv::elem_bytes(dtype);
     if (!p) return fail(SEKV_ERR_INVALID_ARG, "%s is NULL", name);
     if (misaligned(p, 16)) return fail(SEKV_ERR_INVALID_ARG, "%s not 16-byte aligned", name);
-    if (stride < int64_t(heads) * d->head_dim || stride % (16 / e))
+    if (stride < int64_t(heads) * head_dim || stride % (16 / e))
         return fail(SEKV_ERR_INVALID_ARG, "%s: a token stride of %lld elements (at least %d, in 16-byte steps)", name,
-                    (long long)stride, heads * d->head_dim);
+                    (long long)stride, heads * head_dim);
     return SEKV_OK;
+}
+sekv_status check_rows(const sekv_page_dims *d, const void *p, int64_t stride, int heads, const char *name) {
+    return check_rows(d->dtype, d->head_dim, p, stride, heads, name);
+}
+
+// Rows that are turned, and where to: apart, or the same rows.
+sekv_status check_turned(int dtype, int head_dim, const void *x, int64_t x_stride, const void *y, int64_t y_stride,
+                         int heads, const char *x_name, const char *y_name) {
+    sekv_status st = check_rows(dtype, head_dim, x, x_stride, heads, x_name);
+    if (st != SEKV_OK) return st;
+    if ((st = check_rows(dtype, head_dim, y, y_stride, heads, y_name)) != SEKV_OK) return st;
+    if (x == y && x_stride != y_stride)
+        return fail(SEKV_ERR_INVALID_ARG, "%s is %s with another token stride", y_name, x_name);
+    return SEKV_OK;
+}
+
+sekv::RotaryArgs rotary_args(const sekv_rotary *r, int n_tokens, const int32_t *positions) {
+    sekv::RotaryArgs a{};
+    a.t.n_tokens = n_tokens;
+    a.positions = positions;
+    a.freq = r->freq;
+    a.scale = r->scale;
+    a.rot_dim = r->rot_dim;
+    return a;
 }
 
 sekv::PageTables tables(const sekv_page_dims *d, const sekv_pages *p, const int32_t *tok_start, int n_tokens,
@@ -119,6 +143,68 @@ sekv_status sekv_page_append(const sekv_page_dims *dims, const sekv_pages *pages
     a.pool[0] = pages->k; a.pool[1] = pages->v;
     a.scale[0] = pages->k_scale; a.scale[1] = pages->v_scale;
     const hipError_t e = sekv::launch_page_append(a, dims->dtype, dims->page_dtype, dims->head_dim, stream);
+    if (e != hipSuccess) return fail(SEKV_ERR_HIP, "page append launch: %s", hipGetErrorString(e));
+    return SEKV_OK;
+}
+
+sekv_status sekv_rotary_frequencies(const sekv_rotary_spec *spec, double *freq, double *scale) {
+    return sekv::rotary_frequencies(spec, freq, scale);
+}
+
+sekv_status sekv_rotate(const sekv_rotary *rotary, int32_t n_tokens, int32_t n_heads, int32_t head_dim, int32_t dtype,
+                        const void *x, int64_t x_stride, void *y, int64_t y_stride, const int32_t *positions,
+                        int32_t transpose, hipStream_t stream) {
+    if (n_tokens < 0 || n_heads < 1) return fail(SEKV_ERR_INVALID_ARG, "n_tokens < 0 or n_heads < 1");
+    if (head_dim != 64 && head_dim != 128) return fail(SEKV_ERR_UNSUPPORTED, "head_dim %d not in {64,128}", head_dim);
+    if (dtype != SEKV_F32 && dtype != SEKV_BF16) return fail(SEKV_ERR_UNSUPPORTED, "dtype %d", dtype);
+    if (n_heads > 4096) return fail(SEKV_ERR_UNSUPPORTED, "n_heads %d > 4096", n_heads);
+    if (transpose != 0 && transpose != 1) return fail(SEKV_ERR_INVALID_ARG, "transpose is 0 or 1");
+    sekv_status st = sekv::check_rotary(rotary, head_dim);
+    if (st != SEKV_OK || n_tokens == 0) return st;
+    if ((st = check_turned(dtype, head_dim, x, x_stride, y, y_stride, n_heads, "x", "y")) != SEKV_OK) return st;
+    if (!positions || misaligned(positions, 4))
+        return fail(SEKV_ERR_INVALID_ARG, "positions is NULL or not 4-byte aligned");
+    sekv::RotaryArgs a = rotary_args(rotary, n_tokens, positions);
+    a.transpose = transpose;
+    a.Hq = n_heads;
+    a.q = x; a.q_stride = x_stride;
+    a.q_out = y; a.out_stride = y_stride;
+    const hipError_t e = sekv::launch_rotary(a, rotary->layout, dtype, -1, head_dim, stream);
+    if (e != hipSuccess) return fail(SEKV_ERR_HIP, "rotation launch: %s", hipGetErrorString(e));
+    return SEKV_OK;
+}
+
+sekv_status sekv_page_append_rotary(const sekv_page_dims *dims, const sekv_pages *pages, const sekv_rotary *rotary,
+                                    const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, const void *k,
+                                    const void *v, int64_t k_stride, int64_t v_stride, const int32_t *positions,
+                                    const int32_t *tok_start, int32_t n_tokens, void *ws, size_t ws_bytes,
+                                    hipStream_t stream) {
+    if (n_tokens < 0) return fail(SEKV_ERR_INVALID_ARG, "n_tokens < 0");
+    bool go = false;
+    sekv_status st = check_call(dims, pages, ws, ws_bytes, sizeof(sekv::WsHeader), n_tokens == 0, &go);
+    if (st != SEKV_OK) return st;
+    if ((st = sekv::check_rotary(rotary, dims->head_dim)) != SEKV_OK || !go) return st;
+    if (!tok_start || misaligned(tok_start, 4))
+        return fail(SEKV_ERR_INVALID_ARG, "tok_start is NULL or not 4-byte aligned");
+    if (misaligned(positions, 4)) return fail(SEKV_ERR_INVALID_ARG, "positions not 4-byte aligned");
+    if ((st = check_rows(dims, k, k_stride, dims->n_kv_heads, "k")) != SEKV_OK) return st;
+    if ((st = check_rows(dims, v, v_stride, dims->n_kv_heads, "v")) != SEKV_OK) return st;
+    if (!q != !q_out) return fail(SEKV_ERR_INVALID_ARG, "q and q_out are given together or not at all");
+    if (q && (st = check_turned(dims->dtype, dims->head_dim, q, q_stride, q_out, q_out_stride, dims->n_q_heads, "q",
+                                "q_out")) != SEKV_OK)
+        return st;
+    if (int64_t(n_tokens) * dims->n_q_heads > 0x7fffffffll)
+        return fail(SEKV_ERR_UNSUPPORTED, "%d new tokens of %d heads in one call", n_tokens, dims->n_q_heads);
+    sekv::RotaryArgs a = rotary_args(rotary, n_tokens, positions);
+    a.t = tables(dims, pages, tok_start, n_tokens, ws);
+    a.Hq = q ? dims->n_q_heads : 0;
+    a.q = q; a.q_stride = q_stride;
+    a.q_out = q_out; a.out_stride = q_out_stride;
+    a.kv.src[0] = k; a.kv.src[1] = v;
+    a.kv.stride[0] = k_stride; a.kv.stride[1] = v_stride;
+    a.kv.pool[0] = pages->k; a.kv.pool[1] = pages->v;
+    a.kv.scale[0] = pages->k_scale; a.kv.scale[1] = pages->v_scale;
+    const hipError_t e = sekv::launch_rotary(a, rotary->layout, dims->dtype, dims->page_dtype, dims->head_dim, stream);
     if (e != hipSuccess) return fail(SEKV_ERR_HIP, "page append launch: %s", hipGetErrorString(e));
     return SEKV_OK;
 }

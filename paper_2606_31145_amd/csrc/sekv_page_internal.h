@@ -35,6 +35,22 @@ struct PageAppendArgs {
     uint8_t *scale[2];
 };
 
+// Rows turned by their positions: queries to q_out, and for a paged store keys, with values as they are, into the pools.
+struct RotaryArgs {
+    PageTables t;              // n_tokens; the rest for a paged store
+    const int32_t *positions;  // [n_tokens], or null: a token's own in its sequence
+    const double *freq;        // [rot_dim / 2]
+    double scale;
+    int32_t rot_dim, transpose;
+    int32_t Hq;                // 0: no queries
+    const void *q;             // [n_tokens][Hq][d]
+    int64_t q_stride;
+    void *q_out;
+    int64_t out_stride;
+    PageAppendArgs kv;         // a paged store's; its t is not read
+    int32_t chunks, per;       // a token's heads in chunks of so many
+};
+
 struct PageReadArgs {
     PageTables t;
     const void *pool[2];
@@ -68,6 +84,8 @@ hipError_t ws_prepare_pages(void *ws, size_t bytes, size_t words, hipStream_t st
 
 hipError_t launch_zero_words(void *p, size_t words, hipStream_t stream);
 hipError_t launch_page_append(const PageAppendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);
+// page_dtype -1: no pages
+hipError_t launch_rotary(RotaryArgs a, int layout, int dtype, int page_dtype, int head_dim, hipStream_t stream);
 hipError_t launch_page_read(const PageReadArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);
 hipError_t launch_page_attend(const PageAttendArgs &a, int dtype, int page_dtype, int head_dim, hipStream_t stream);
 

@@ -36,7 +36,8 @@ EXPORTED = ("sekv_status_string", "sekv_last_error", "sekv_phase_trace", "sekv_c
             "sekv_decode_step_gated", "sekv_segment_workspace_size", "sekv_segment",
             "sekv_build_layout", "sekv_build_cache", "sekv_decode_layers_tiered",
             "sekv_tier_layer_stats", "sekv_check_page_dims", "sekv_page_workspace_size",
-            "sekv_page_append", "sekv_page_read", "sekv_page_attend")
+            "sekv_page_append", "sekv_page_read", "sekv_page_attend", "sekv_rotary_frequencies", "sekv_rotate",
+            "sekv_page_append_rotary")
 
 
 class SekvError(RuntimeError):
@@ -100,6 +101,17 @@ class PagesStruct(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
                 ("seq_len", ctypes.c_void_p)]
+
+
+class RotaryStruct(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("freq", ctypes.c_void_p),
+                ("scale", ctypes.c_double)]
+
+
+class RotarySpec(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("trained", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double)]
 
 
 def _load():
@@ -175,6 +187,15 @@ def _load():
     lib.sekv_page_append.restype = ctypes.c_int
     lib.sekv_page_append.argtypes = [P(PageDims), P(PagesStruct), VP, VP, ctypes.c_int64, ctypes.c_int64, VP,
                                      ctypes.c_int32, VP, SZ, VP]
+    lib.sekv_rotary_frequencies.restype = ctypes.c_int
+    lib.sekv_rotary_frequencies.argtypes = [P(RotarySpec), VP, P(ctypes.c_double)]
+    lib.sekv_rotate.restype = ctypes.c_int
+    lib.sekv_rotate.argtypes = [P(RotaryStruct), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, VP,
+                                ctypes.c_int64, VP, ctypes.c_int64, VP, ctypes.c_int32, VP]
+    lib.sekv_page_append_rotary.restype = ctypes.c_int
+    lib.sekv_page_append_rotary.argtypes = [P(PageDims), P(PagesStruct), P(RotaryStruct), VP, ctypes.c_int64, VP,
+                                            ctypes.c_int64, VP, VP, ctypes.c_int64, ctypes.c_int64, VP, VP,
+                                            ctypes.c_int32, VP, SZ, VP]
     lib.sekv_page_read.restype = ctypes.c_int
     lib.sekv_page_read.argtypes = [P(PageDims), P(PagesStruct), VP, VP, ctypes.c_int32, VP, SZ, VP]
     lib.sekv_page_attend.restype = ctypes.c_int
@@ -797,8 +818,12 @@ def _expect(x, name, dtype, shape, device):
 
 def _token_rows(pd: PageDims, x, name, heads, device):
     """(address, token stride) of [n_tokens][heads][d] rows that are contiguous within a token."""
-    d, n = pd.head_dim, x.shape[0]
-    _expect(x, name, _PAGE_STORAGE[pd.dtype], (n, heads, d), device)
+    return _rows_of(_PAGE_STORAGE[pd.dtype], pd.head_dim, x, name, heads, device)
+
+
+def _rows_of(dtype, d, x, name, heads, device):
+    n = x.shape[0]
+    _expect(x, name, dtype, (n, heads, d), device)
     s = x.stride()
     if n and (s[2] != 1 or (heads > 1 and s[1] != d)):
         raise ValueError(f"{name}: a token's heads have to lie one after another")
@@ -813,18 +838,18 @@ def _tok_start(pd: PageDims, tok_start, device):
 _HERE = contextlib.nullcontext()
 
 
-def _on(device, stream):
+def _on(device, stream, what="pages"):
     """The device and stream context of a call, and the stream's handle: the caller's stream, else the
     device's current one."""
     if device.type != "cuda":
-        raise ValueError("the pages have to be on a GPU")
+        raise ValueError(f"the {what} have to be on a GPU")
     if stream is None:
         st = torch._C._cuda_getCurrentRawStream(device.index)
         return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device), st
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     if stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, the pages on {device}")
+        raise ValueError(f"the stream is on {stream.device}, the {what} on {device}")
     return torch.cuda.stream(stream), stream.cuda_stream
 
 
@@ -846,6 +871,99 @@ def page_append(pd: PageDims, cache: PageCache, k, v, tok_start, ws: Workspace, 
     ctx, st = _on(dev, stream)
     with ctx:
         _check(LIB.sekv_page_append(pd, cs, kp, vp, sk, sv, ts, len(k), *_page_ws(ws, dev), st))
+
+
+_ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+_ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def rotary_frequencies(rot_dim: int, base: float, scaling: str = "plain", *, factor=1.0, trained=0.0, low=1.0,
+                       high=32.0):
+    """sekv_rotary_frequencies: (radians a position float64 [rot_dim / 2] on the host, scale of the turned values)."""
+    spec = RotarySpec(int(rot_dim), _ROTARY_SCALINGS[scaling], float(base), float(factor), float(trained), float(low),
+                      float(high))
+    freq = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.float64)
+    scale = ctypes.c_double(0.0)
+    _check(LIB.sekv_rotary_frequencies(ctypes.byref(spec), freq.ctypes.data, ctypes.byref(scale)))
+    return torch.from_numpy(freq), float(scale.value)
+
+
+class Rotary:
+    """Rotary positions as sekv_rotary describes them: freq float64 [rot_dim / 2] on the device of the rows (the
+    tensor is kept), layout "half" or "interleaved", scale of the turned values."""
+
+    def __init__(self, freq, layout: str = "half", scale: float = 1.0):
+        if not isinstance(freq, torch.Tensor) or freq.dtype != torch.float64 or freq.dim() != 1:
+            raise ValueError("freq: a float64 tensor [rot_dim / 2]")
+        self.freq = freq.contiguous()
+        self._struct = RotaryStruct(2 * len(freq), _ROTARY_LAYOUTS[layout], self.freq.data_ptr(), float(scale))
+
+    @property
+    def rot_dim(self) -> int:
+        return self._struct.rot_dim
+
+    def struct(self, device) -> RotaryStruct:
+        if self.freq.device != device:
+            raise ValueError(f"the frequencies are on {self.freq.device}, the rows on {device}")
+        return self._struct
+
+
+def _positions(positions, n, device):
+    if positions is None:
+        return None
+    _expect(positions, "positions", torch.int32, (n,), device)
+    return _ptr(positions)
+
+
+def rotate(x, positions, rotary: Rotary, out=None, transpose: bool = False, stream=None):
+    """sekv_rotate: x [n_tokens][heads][d] (tokens may be strided; float32 or bfloat16) turned by positions int32
+    [n_tokens]; out may be x itself.  transpose: the other way, which is the gradient with respect to x."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 3 or x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("x: float32 or bfloat16 [n_tokens][heads][d]")
+    n, heads, d = x.shape
+    dev = x.device
+    xp, sx = _rows_of(x.dtype, d, x, "x", heads, dev)
+    if positions is None:
+        raise ValueError("positions are needed")
+    pp, rs = _positions(positions, n, dev), rotary.struct(dev)
+    ctx, st = _on(dev, stream, "rows")
+    with ctx:
+        if out is None:
+            out = torch.empty((n, heads, d), dtype=x.dtype, device=dev)
+        yp, sy = _rows_of(x.dtype, d, out, "out", heads, dev)
+        if len(out) != n:
+            raise ValueError(f"out: {len(out)} tokens, x has {n}")
+        _check(LIB.sekv_rotate(rs, n, heads, d, SEKV_F32 if x.dtype == torch.float32 else SEKV_BF16, xp, sx, yp, sy, pp,
+                               int(bool(transpose)), st))
+    return out
+
+
+def page_append_rotary(pd: PageDims, cache: PageCache, rotary: Rotary, q, k, v, tok_start, ws: Workspace, q_out=None,
+                       positions=None, stream=None):
+    """sekv_page_append_rotary: stores k turned by its positions and v [n_tokens][Hkv][d] in the pages, and returns
+    q [n_tokens][Hq][d] turned likewise (None without q).  q_out may be q itself; rows that belong to no sequence
+    are left as given, undefined in a tensor allocated here.  positions int32 [n_tokens]; None: the tokens' own in
+    their sequences."""
+    cs, dev = cache.struct(pd), cache.k_pages.device
+    kp, sk = _token_rows(pd, k, "k", pd.n_kv_heads, dev)
+    vp, sv = _token_rows(pd, v, "v", pd.n_kv_heads, dev)
+    n = len(k)
+    if len(v) != n:
+        raise ValueError(f"v: {len(v)} tokens, k has {n}")
+    qp, sq = (None, 0) if q is None else _token_rows(pd, q, "q", pd.n_q_heads, dev)
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    ts, pp, rs = _tok_start(pd, tok_start, dev), _positions(positions, n, dev), rotary.struct(dev)
+    ctx, st = _on(dev, stream)
+    with ctx:
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        op, so = (None, 0) if q is None else _token_rows(pd, q_out, "q_out", pd.n_q_heads, dev)
+        for name, x in (("q", q), ("q_out", q_out)):
+            if x is not None and len(x) != n:
+                raise ValueError(f"{name}: {len(x)} tokens, k has {n}")
+        _check(LIB.sekv_page_append_rotary(pd, cs, rs, qp, sq, op, so, kp, vp, sk, sv, pp, ts, n, *_page_ws(ws, dev), st))
+    return q_out
 
 
 def page_read(pd: PageDims, cache: PageCache, max_tokens: int, ws: Workspace, keys=None, values=None, stream=None):
