@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
                 (s.nq && a.t.seq_len[b] > cap))
                 flag(a.t);
         }
-    const Plan plan = make_plan(a, T::kBytes == 4, lane, lds);
+    const Plan plan = make_plan(a, T::kBytes == 4, P::kBytes == 0, lane, lds);
     int b = 0, c = 0, g = 0;
     const uint32_t x = place_of(blockIdx.x, a.t.Hkv, &g);
     Item it;
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
     constexpr int kParts = join_parts(D), kRows = kTileRows / kParts;
     __shared__ __attribute__((aligned(16))) unsigned char lds[256 * (sizeof(float4) + sizeof(float2))];
     const int lane = threadIdx.x & 63;
-    const Plan plan = make_plan(a, T::kBytes == 4, lane, lds);
+    const Plan plan = make_plan(a, T::kBytes == 4, false, lane, lds);
     if (!plan.chunk || plan.longest <= plan.chunk) return;   // nothing was cut
     const int64_t all = int64_t(plan.tiles) * a.t.Hkv * kParts;
     for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {

@@ -50,6 +50,11 @@ SEKV_HD int over_of(bool wide, bool is_float) { return wide && !is_float ? kOver
 SEKV_HD float join_rows_of(bool wide, int n_tokens, int group_shift, int T) {
     return wide || T < 1 ? 0.f : float(int64_t(n_tokens) << group_shift) / float(T);
 }
+// 4-bit keys whose partials the last workgroup of a tile joins: a key takes less time, so an item and a join cost more
+// keys.  Measured (us) with 128 and 1 and with these: one token over 8192 keys 16.5, 13.1, over 32768 23.0, 21.3, of 32
+// ragged sequences of up to 2000 27.0, 23.6, of 8 of up to 9000 27.7, 25.1.
+constexpr int kOver4 = 256;
+constexpr float kJoin4 = 4.f;
 constexpr int kBlock = 16;         // keys that lie in one page: the smallest page
 
 // Pool row of position `pos` (below max_pages * page_size) from its table entry; -1 when the page is

@@ -95,7 +95,7 @@ __device__ inline uint32_t block_exponent(uint32_t top) {
     const int E = int(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u ? 1 : 0);
     return top >= 0x7f800000u ? 255u : top == 0 ? 127u : uint32_t(E < 2 ? 2 : E > 252 ? 252 : E);
 }
-// the codes of byte i of w
+// the codes of byte I of w
 template <int I>
 __device__ inline uint32_t pair_bf16(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, I));
@@ -106,6 +106,16 @@ __device__ inline void pair_f32(uint32_t w, float scale, float &x, float &y) {
     const f2 r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, I);
     x = r[0];
     y = r[1];
+}
+// byte i of a word, i a constant after unrolling
+__device__ inline uint32_t word_pair(uint32_t w, float scale, int i) {
+    return i == 0 ? pair_bf16<0>(w, scale) : i == 1 ? pair_bf16<1>(w, scale) : i == 2 ? pair_bf16<2>(w, scale) : pair_bf16<3>(w, scale);
+}
+__device__ inline void word_pair(uint32_t w, float scale, int i, float &x, float &y) {
+    if (i == 0) pair_f32<0>(w, scale, x, y);
+    else if (i == 1) pair_f32<1>(w, scale, x, y);
+    else if (i == 2) pair_f32<2>(w, scale, x, y);
+    else pair_f32<3>(w, scale, x, y);
 }
 // eight codes
 __device__ inline uint4 word_bf16(uint32_t w, float scale) {

@@ -95,7 +95,7 @@ struct Plan {
 };
 
 // lds: 256 bytes, free again on return.
-__device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, int lane, unsigned char *lds) {
+__device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, bool four, int lane, unsigned char *lds) {
     Plan p;
     uint64_t W = 0;
     int mx = 0, T = 0;
@@ -150,8 +150,9 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, int lan
     W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
     p.tiles = __builtin_amdgcn_readfirstlane(T);
     p.longest = __builtin_amdgcn_readfirstlane(mx);
-    p.chunk = chunk_length(W, p.tiles, p.longest, a.t.Hkv, a.target, a.splits, over_of(a.join_launch, is_float),
-                           join_rows_of(a.join_launch, a.t.n_tokens, a.group_shift, p.tiles));
+    const float rows = join_rows_of(a.join_launch, a.t.n_tokens, a.group_shift, p.tiles);
+    p.chunk = chunk_length(W, p.tiles, p.longest, a.t.Hkv, a.target, a.splits,
+                           four && !a.join_launch ? kOver4 : over_of(a.join_launch, is_float), four ? kJoin4 * rows : rows);
     return p;
 }
 
@@ -310,8 +311,7 @@ struct Keys16 {
     static constexpr int kBlocks = T::kBytes == 2 ? 2 : 1, kKeys = 16 * kBlocks;
     static constexpr int kRow = P::row(D);
     static constexpr int KW = kRow / 16, VW = kRow >= 64 ? kRow / 64 : 1;     // words a lane
-    static constexpr int SW = P::kBytes == 0 ? P::scales(D) : 1;              // words of the exponent bytes of four rows
-    uint32_t k[kBlocks][KW], v[kBlocks][4][VW], ks[kBlocks], vs[kBlocks][SW];
+    uint32_t k[kBlocks][KW], v[kBlocks][4][VW], ks[kBlocks], vs[kBlocks];
 
     __device__ static size_t base(int row) { return row >= 0 ? row : 0; }     // any row: its keys are masked
     __device__ void load_keys(const PageAttendArgs &a, const int (&row)[kBlocks], int lane) {
@@ -358,30 +358,20 @@ struct Keys16 {
                     v[j][i][0] = *reinterpret_cast<const uint32_t *>(p);
                 }
             }
-            if constexpr (P::kBytes == 1) vs[j][0] = *reinterpret_cast<const uint32_t *>(a.v_scale + r0 + 4 * g);
-            if constexpr (P::kBytes == 0) {
-                const uint32_t *s = reinterpret_cast<const uint32_t *>(a.v_scale + (r0 + 4 * g) * SW);
-                if constexpr (SW == 4) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(s);
-                    vs[j][0] = w.x; vs[j][1] = w.y; vs[j][2] = w.z; vs[j][3] = w.w;
-                } else {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(s);
-                    vs[j][0] = w.x; vs[j][1] = w.y;
-                }
-            }
+            if constexpr (P::kBytes == 1) vs[j] = *reinterpret_cast<const uint32_t *>(a.v_scale + r0 + 4 * g);
+            // a quad of lanes holds values of one block of four rows: each lane one row's exponent byte.  All four
+            // rows' words in every lane cost one token of 32 sequences of up to 32768 209 us instead of 169.
+            if constexpr (P::kBytes == 0) vs[j] = a.v_scale[(r0 + 4 * g + (m & 3)) * P::scales(D) + m * P::scales(D) / 16];
         }
     }
-    // Exponent byte of the values that the lane holds of row 4 g + i of block j; that of a row that counts as zeros.
-    __device__ static int shift(int i, int lane) {
-        const int m = lane & 15;
-        return P::kBytes == 1 ? 8 * i : SW == 4 ? 8 * (m >> 2) : 16 * (i & 1) + 8 * (m >> 3);
+    // Exponent byte of the values that the lane holds of row 4 g + i of block j.
+    template <int I>
+    __device__ uint32_t row_scale(int j) const {
+        if constexpr (P::kBytes == 0) return __builtin_amdgcn_mov_dpp(vs[j], 0x55 * I, 0xf, 0xf, true);   // lane I of the quad
+        else return vs[j] >> (8 * I) & 255u;
     }
-    __device__ uint32_t scale(int j, int i, int lane) const {
-        return vs[j][P::kBytes == 1 ? 0 : SW == 4 ? i : i >> 1] >> shift(i, lane) & 255u;
-    }
-    __device__ void drop_scale(int j, int i, int lane) {
-        uint32_t &w = vs[j][P::kBytes == 1 ? 0 : SW == 4 ? i : i >> 1];
-        w = (w & ~(255u << shift(i, lane))) | 127u << shift(i, lane);
+    __device__ uint32_t scale(int j, int i) const {
+        return i == 0 ? row_scale<0>(j) : i == 1 ? row_scale<1>(j) : i == 2 ? row_scale<2>(j) : row_scale<3>(j);
     }
 };
 
@@ -559,6 +549,11 @@ struct Rows16 {
     // holds an infinity or NaN, or 8-bit values that may become one: zero times that is no number.
     __device__ void values(Tile &t, const f4v (&s)[J][NB], int pos, uint32_t valid, bool part, bool *bad, int lane) {
         const int g = lane >> 4;
+        uint32_t vs[J][4];                                    // exponent bytes
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vs[j][i] = P::kBytes <= 1 ? t.scale(j, i) : 0u;
         if (part) {
 #pragma unroll
             for (int j = 0; j < J; ++j)
@@ -569,8 +564,8 @@ struct Rows16 {
                     uint32_t wrong = 0;
                     // the exponent byte as well: one of 255 makes no number of any code
                     if constexpr (P::kBytes <= 1) {
-                        if (!keep) t.drop_scale(j, i, lane);
-                        wrong = uint32_t(t.scale(j, i, lane) >= (P::kBytes == 1 ? kOverExponent : kOverExponent4));
+                        vs[j][i] = keep ? vs[j][i] : 127u;
+                        wrong = uint32_t(vs[j][i] >= (P::kBytes == 1 ? kOverExponent : kOverExponent4));
                     }
 #pragma unroll
                     for (int w = 0; w < Tile::VW; ++w) {
@@ -596,8 +591,8 @@ struct Rows16 {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (P::kBytes == 2) x[j][i] = t.v[j][i][w];
-                        else if constexpr (P::kBytes == 1) x[j][i] = codes2_bf16(t.v[j][i][w / 2], pow2_of(t.scale(j, i, lane)), w & 1);
-                        else x[j][i] = pair_bf16<0>(t.v[j][i][0] >> (8 * w), pow2_of(t.scale(j, i, lane)));
+                        else if constexpr (P::kBytes == 1) x[j][i] = codes2_bf16(t.v[j][i][w / 2], pow2_of(vs[j][i]), w & 1);
+                        else x[j][i] = word_pair(t.v[j][i][0], pow2_of(vs[j][i]), w);
                     }
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -618,13 +613,12 @@ struct Rows16 {
                     for (int e = 0; e < VE; ++e) vf[e] = __uint_as_float(t.v[0][i][e]);
                 } else if constexpr (P::kBytes == 0) {
 #pragma unroll
-                    for (int w = 0; w < VE / 2; ++w)
-                        pair_f32<0>(t.v[0][i][0] >> (8 * w), pow2_of(t.scale(0, i, lane)), vf[2 * w], vf[2 * w + 1]);
+                    for (int w = 0; w < VE / 2; ++w) word_pair(t.v[0][i][0], pow2_of(vs[0][i]), w, vf[2 * w], vf[2 * w + 1]);
                 } else {
 #pragma unroll
                     for (int w = 0; w < VE / 4; ++w) {
                         float x[4];
-                        codes4_up(t.v[0][i][w], pow2_of(t.scale(0, i, lane)), x);
+                        codes4_up(t.v[0][i][w], pow2_of(vs[0][i]), x);
 #pragma unroll
                         for (int u = 0; u < 4; ++u) vf[4 * w + u] = x[u];
                     }
@@ -641,8 +635,9 @@ struct Rows16 {
     // A group's keys and values are asked for as soon as the registers of an earlier one are free, kAhead groups
     // ahead; its row blocks one group before that.  Two groups where they fit: 32 ragged sequences in bfloat16 462 us
     // against 469 with one, 4 of 131072 in 8 bits 188.6 against 191.2, 13 of float and head_dim 64 577 against 599.
-    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 1 + Tile::SW : 0)), kHeld = NB * (D / 4 + QW);
-    static constexpr int kAhead = 2 * kTileWords + kHeld <= 176 ? 2 : 1;      // of 256 registers
+    // In 4 bits three: 32 ragged sequences 168.7 us against 173.4 with two, 167.8 with four, 4 of 131072 109.9, 109.5, 110.6.
+    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 2 : 0)), kHeld = NB * (D / 4 + QW);
+    static constexpr int kAhead = P::kBytes == 0 ? 3 : 2 * kTileWords + kHeld <= 176 ? 2 : 1;     // of 256 registers
     __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int step, bool *bad, int lane) {
         if (pos >= it.end) return;
         Tile t[kAhead];

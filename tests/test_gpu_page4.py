@@ -209,6 +209,12 @@ ATTENDS = [
     dict(lens=[1500, 1400], news=[12, 3], group=4, kv_heads=1, dim=128, page=64, window=700),
     dict(lens=[900, 64], news=[64, 64], group=1, kv_heads=4, dim=128, page=32),
     dict(lens=[777], news=[200], group=8, kv_heads=1, dim=64, page=64),
+    # no more tokens than sequences: one each, and all of them in a few
+    dict(lens=[9000, 5000, 7777, 8192, 6001, 9000, 9000, 8999], news=[1] * 8, kv_heads=8, dim=128, page=64),
+    dict(lens=[4100, 3900, 4097, 4000] * 5, news=[1] * 20, kv_heads=4, group=8, dim=64, page=16),
+    dict(lens=[700] + [20] * 39, news=[40] + [0] * 39, group=4, dim=128, page=32),
+    dict(lens=[700, 90] + [20] * 58, news=[40, 17] + [0] * 57 + [1], group=8, kv_heads=1, dim=64, page=16, window=300),
+    dict(lens=[60, 900] + [0] * 9, news=[5, 6] + [0] * 9, group=8, kv_heads=3, dim=128, page=16),
 ]
 
 
@@ -227,7 +233,8 @@ def test_attend_skips_bad_pages(S, dtype):
         _check_attend(S, c, bits=8)
 
 
-SHAPES = [([1, 1], 4, 128), ([6, 3], 4, 64), ([9, 2], 4, 128), ([40, 6], 4, 128), ([150, 33], 1, 128), ([150, 33], 1, 64)]
+FEW = [0] * 70       # empty sequences beside: no more tokens than sequences
+SHAPES = [([1, 1], 4, 128), ([40, 6] + FEW, 4, 128), ([9, 2] + FEW, 8, 64), ([6, 3], 4, 64), ([9, 2], 4, 128), ([40, 6], 4, 128), ([150, 33], 1, 128), ([150, 33], 1, 64)]
 
 
 def _hidden(c):
@@ -248,7 +255,8 @@ def _hidden(c):
 def test_rows_that_nobody_sees(S, dtype, news, group, dim, window, exponent, code):
     """Every row that no query sees holds bytes that decode to NaN or infinities: the results are those without."""
     banner(f"unseen e2m1 {dtype} {news} {group} {dim} {window} {exponent} {code}")
-    c = Case4(dtype, [200, 77], news, group=group, dim=dim, page=32, window=window, seed=_seed(dtype, news, group, dim))
+    c = Case4(dtype, [200, 77] + [0] * (len(news) - 2), news, group=group, dim=dim, page=32, window=window,
+              seed=_seed(dtype, news, group, dim))
     used = set(c.table[c.table < c.n_pages].tolist())
     if 0 in used:                                    # page 0 stands in where a block holds no key
         free = next(p for p in range(c.n_pages) if p not in used)
@@ -271,7 +279,7 @@ def test_nan_blocks_reach_those_who_see_them(S, dtype, news, group, dim, window)
     """One block of NaN in a value row that some of a chunk's queries see: the others have their value, and so
     have the other columns of those who see it.  In a key row all columns of those who see it are NaN."""
     banner(f"nan block {dtype} {news} {group} {dim} {window}")
-    lens = [200, 77]
+    lens = [200, 77] + [0] * (len(news) - 2)
     for which in "vk":
         for b, t in ((0, lens[0] - 1 - news[0] // 2), (1, lens[1] - news[1]), (0, lens[0] - news[0] - 30)):
             if t < 0:
@@ -301,7 +309,7 @@ def test_nan_blocks_reach_those_who_see_them(S, dtype, news, group, dim, window)
 def test_scores_past_two_to_the_26(S, dtype, news, group, dim):
     """Scores too large for the fused step are done row by row: one key wins, and its value comes back."""
     banner(f"large scores e2m1 {dtype} {news} {group} {dim}")
-    c = Case4(dtype, [200, 77], news, group=group, dim=dim, page=32, seed=_seed(news, dim))
+    c = Case4(dtype, [200, 77] + [0] * (len(news) - 2), news, group=group, dim=dim, page=32, seed=_seed(news, dim))
     for name in "k":
         c.codes[name][1].fill_(127 + 24)
         c.pools[name] = decode4(*c.codes[name])
@@ -335,6 +343,37 @@ def test_same_bits_again_and_on_another_stream(S, dtype):
     b, lb = S.page_attend(c.dims(S), cache, q, ts, ws, want_lse=True, stream=st)
     st.synchronize()
     assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+def test_many_items_repeat_and_replay(S):
+    """More items than run at once: the same bits call after call, on a workspace that other shapes use between, and in a
+    captured graph whose lengths change."""
+    c = Case4("bf16", [4000 + 7 * b for b in range(40)], [1] * 40, dim=64, kv_heads=8, group=2, page=64, seed=6)
+    d = Case4("bf16", [900, 31], [1, 1], dim=64, kv_heads=8, group=2, page=64, seed=7)
+    cache, q, ts, ws = c.cache(S), c.q.cuda(), c.tok_start(), c.workspace(S)
+    other = d.cache(S), d.q.cuda(), d.tok_start()
+    want = S.page_attend(c.dims(S), cache, q, ts, ws, want_lse=True)
+    ref, rl, tol, ltol = c.attend()
+    assert ((want[0].cpu().double() - ref).abs() <= tol).all() and ((want[1].cpu().double() - rl).abs() <= ltol).all()
+    small = S.page_attend(d.dims(S), *other[:2], other[2], ws, want_lse=True)
+    out, lse = torch.empty_like(want[0]), torch.empty_like(want[1])
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        S.page_attend(c.dims(S), cache, q, ts, ws, out=out, lse=lse)
+    lens = cache.seq_len.clone()
+    for turn in range(6):
+        got = S.page_attend(c.dims(S), cache, q, ts, ws, want_lse=True)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        got = S.page_attend(d.dims(S), *other[:2], other[2], ws, want_lse=True)
+        assert torch.equal(got[0], small[0]) and torch.equal(got[1], small[1])
+        cache.seq_len.copy_(lens - 500 * turn)
+        out.fill_(7.0)
+        gr.replay()
+        eager = S.page_attend(c.dims(S), cache, q, ts, ws, want_lse=True)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+        cache.seq_len.copy_(lens)
+    assert ws.status() == 0
 
 
 def test_one_workspace_for_all_storages(S):
