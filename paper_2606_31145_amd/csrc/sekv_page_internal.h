@@ -48,7 +48,8 @@ struct RotaryArgs {
     void *q_out;
     int64_t out_stride;
     PageAppendArgs kv;         // a paged store's; its t is not read
-    int32_t chunks, per;       // a token's heads in chunks of so many
+    int32_t kv_chunks, kv_per, q_chunks, q_per;      // a token's heads in chunks of so many (queries: of rows side by side)
+    int64_t kv_items, q_items; // a wave's work each, the keys first
 };
 
 struct PageReadArgs {

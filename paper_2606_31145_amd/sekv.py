@@ -818,21 +818,29 @@ def _expect(x, name, dtype, shape, device):
 
 def _token_rows(pd: PageDims, x, name, heads, device):
     """(address, token stride) of [n_tokens][heads][d] rows that are contiguous within a token."""
-    return _rows_of(_PAGE_STORAGE[pd.dtype], pd.head_dim, x, name, heads, device)
+    return _rows_of(_PAGE_STORAGE[pd.dtype], pd.head_dim, x, name, heads, device)[1:]
 
 
 def _rows_of(dtype, d, x, name, heads, device):
+    """(n_tokens, address, token stride)"""
     n = x.shape[0]
-    _expect(x, name, dtype, (n, heads, d), device)
+    if x.dtype is not dtype or x.shape != (n, heads, d) or x.device != device:
+        _expect(x, name, dtype, (n, heads, d), device)
     s = x.stride()
     if n and (s[2] != 1 or (heads > 1 and s[1] != d)):
         raise ValueError(f"{name}: a token's heads have to lie one after another")
-    return x.data_ptr(), s[0] if n > 1 else heads * d
+    return n, x.data_ptr(), s[0] if n > 1 else heads * d
 
 
 def _tok_start(pd: PageDims, tok_start, device):
-    _expect(tok_start, "tok_start", torch.int32, (pd.batch + 1,), device)
-    return _ptr(tok_start)
+    return _ints(tok_start, "tok_start", pd.batch + 1, device)
+
+
+def _ints(x, name, n, device):
+    """Address of an int32 [n] tensor."""
+    if not isinstance(x, torch.Tensor) or x.dtype is not torch.int32 or x.shape != (n,) or x.device != device:
+        _expect(x, name, torch.int32, (n,), device)
+    return _ptr(x)
 
 
 _HERE = contextlib.nullcontext()
@@ -908,33 +916,26 @@ class Rotary:
         return self._struct
 
 
-def _positions(positions, n, device):
-    if positions is None:
-        return None
-    _expect(positions, "positions", torch.int32, (n,), device)
-    return _ptr(positions)
-
-
 def rotate(x, positions, rotary: Rotary, out=None, transpose: bool = False, stream=None):
     """sekv_rotate: x [n_tokens][heads][d] (tokens may be strided; float32 or bfloat16) turned by positions int32
     [n_tokens]; out may be x itself.  transpose: the other way, which is the gradient with respect to x."""
     if not isinstance(x, torch.Tensor) or x.dim() != 3 or x.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("x: float32 or bfloat16 [n_tokens][heads][d]")
-    n, heads, d = x.shape
-    dev = x.device
-    xp, sx = _rows_of(x.dtype, d, x, "x", heads, dev)
+    _, heads, d = x.shape
+    dev, dt = x.device, x.dtype
+    n, xp, sx = _rows_of(dt, d, x, "x", heads, dev)
     if positions is None:
         raise ValueError("positions are needed")
-    pp, rs = _positions(positions, n, dev), rotary.struct(dev)
+    pp, rs = _ints(positions, "positions", n, dev), rotary.struct(dev)
     ctx, st = _on(dev, stream, "rows")
     with ctx:
         if out is None:
-            out = torch.empty((n, heads, d), dtype=x.dtype, device=dev)
-        yp, sy = _rows_of(x.dtype, d, out, "out", heads, dev)
-        if len(out) != n:
-            raise ValueError(f"out: {len(out)} tokens, x has {n}")
-        _check(LIB.sekv_rotate(rs, n, heads, d, SEKV_F32 if x.dtype == torch.float32 else SEKV_BF16, xp, sx, yp, sy, pp,
-                               int(bool(transpose)), st))
+            out = torch.empty((n, heads, d), dtype=dt, device=dev)
+        m, yp, sy = _rows_of(dt, d, out, "out", heads, dev)
+        if m != n:
+            raise ValueError(f"out: {m} tokens, x has {n}")
+        _check(LIB.sekv_rotate(rs, n, heads, d, SEKV_F32 if dt is torch.float32 else SEKV_BF16, xp, sx, yp, sy, pp,
+                               1 if transpose else 0, st))
     return out
 
 
@@ -945,23 +946,25 @@ def page_append_rotary(pd: PageDims, cache: PageCache, rotary: Rotary, q, k, v, 
     are left as given, undefined in a tensor allocated here.  positions int32 [n_tokens]; None: the tokens' own in
     their sequences."""
     cs, dev = cache.struct(pd), cache.k_pages.device
-    kp, sk = _token_rows(pd, k, "k", pd.n_kv_heads, dev)
-    vp, sv = _token_rows(pd, v, "v", pd.n_kv_heads, dev)
-    n = len(k)
-    if len(v) != n:
-        raise ValueError(f"v: {len(v)} tokens, k has {n}")
-    qp, sq = (None, 0) if q is None else _token_rows(pd, q, "q", pd.n_q_heads, dev)
+    dt, d, Hq, Hkv = _PAGE_STORAGE[pd.dtype], pd.head_dim, pd.n_q_heads, pd.n_kv_heads
+    n, kp, sk = _rows_of(dt, d, k, "k", Hkv, dev)
+    nv, vp, sv = _rows_of(dt, d, v, "v", Hkv, dev)
+    if nv != n:
+        raise ValueError(f"v: {nv} tokens, k has {n}")
     if q is None and q_out is not None:
         raise ValueError("q_out without q")
-    ts, pp, rs = _tok_start(pd, tok_start, dev), _positions(positions, n, dev), rotary.struct(dev)
+    nq, qp, sq = (n, None, 0) if q is None else _rows_of(dt, d, q, "q", Hq, dev)
+    if nq != n:
+        raise ValueError(f"q: {nq} tokens, k has {n}")
+    ts, rs = _tok_start(pd, tok_start, dev), rotary.struct(dev)
+    pp = None if positions is None else _ints(positions, "positions", n, dev)
     ctx, st = _on(dev, stream)
     with ctx:
         if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        op, so = (None, 0) if q is None else _token_rows(pd, q_out, "q_out", pd.n_q_heads, dev)
-        for name, x in (("q", q), ("q_out", q_out)):
-            if x is not None and len(x) != n:
-                raise ValueError(f"{name}: {len(x)} tokens, k has {n}")
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        no, op, so = (n, None, 0) if q is None else _rows_of(dt, d, q_out, "q_out", Hq, dev)
+        if no != n:
+            raise ValueError(f"q_out: {no} tokens, k has {n}")
         _check(LIB.sekv_page_append_rotary(pd, cs, rs, qp, sq, op, so, kp, vp, sk, sv, pp, ts, n, *_page_ws(ws, dev), st))
     return q_out
 
