@@ -29,6 +29,21 @@ using namespace page;
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int64_t kJoinBlocks = 2048;      // eight on each compute unit
 
+// __syncthreads_or for a workgroup's one question.  The library's keeps all of a thread's indices in a register until then,
+// which the float form of 4-bit keys does not have to spare.
+__device__ inline bool any_thread(bool x, int lane, int wave) {
+    __shared__ uint32_t told[kWaves];
+    const bool here = __any(x);
+    if (lane == 0) told[wave] = here;
+    __syncthreads();
+    return told[0] | told[1] | told[2] | told[3];
+}
+template <class P>
+__device__ inline bool any_of(bool x, int lane, int wave) {
+    if constexpr (P::kBytes == 0) return any_thread(x, lane, wave);
+    else return __syncthreads_or(x);
+}
+
 // At most 16 NB rows: every wave takes all of them, and every fourth step of the keys.  True when the
 // item has to be done again by plain_rows.
 template <class T, class P, int D, int NB>
@@ -37,7 +52,7 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
     constexpr int VE = R::VE, RS = D + 4, kKeys = R::Tile::kKeys, N = 16 * NB;
     R r;
     r.init(a, it, g, 0, lane);
-    bool bad = false;
+    bool bad = r.odd_scale;
     r.run(a, it, b, g, it.begin + wave * kKeys, kKeys * kWaves, &bad, lane);
     // the four waves' parts, joined through LDS
     float *ml = reinterpret_cast<float *>(lds), *so = ml + kWaves * 2 * N;
@@ -54,7 +69,7 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
 #pragma unroll
             for (int e = 0; e < VE; ++e) so[(wave * N + 16 * nb + n) * RS + VE * (4 * gq + i) + e] = r.o[nb][e][i];
     }
-    if (__syncthreads_or(bad)) return true;
+    if (any_of<P>(bad, lane, wave)) return true;
     const int d0 = (threadIdx.x & 15) * 2;                   // and 32, 64, .. on: what 16 threads store lies together
     for (int rw = threadIdx.x >> 4; rw < it.rows; rw += 16) {
         float m = -INFINITY, sum = 0.f, o[VE / 2][2] = {};
@@ -88,9 +103,10 @@ __device__ inline bool wide_f32(const PageAttendArgs &a, const Item &it, int b, 
     bool bad = false;
     if (wave * 32 < it.rows) {
         r.init(a, it, g, wave * 32, lane);
-        r.run(a, it, b, g, it.begin, 16, &bad, lane);
+        bad = r.odd_scale;
+        r.run(a, it, b, g, it.begin, R::Tile::kKeys, &bad, lane);
     }
-    if (__syncthreads_or(bad)) return true;
+    if (any_of<P>(bad, lane, wave)) return true;
     if (wave * 32 >= it.rows) return false;
     const int n = lane & 15, gq = lane >> 4;
 #pragma unroll

@@ -111,12 +111,6 @@ __device__ inline void pair_f32(uint32_t w, float scale, float &x, float &y) {
 __device__ inline uint32_t word_pair(uint32_t w, float scale, int i) {
     return i == 0 ? pair_bf16<0>(w, scale) : i == 1 ? pair_bf16<1>(w, scale) : i == 2 ? pair_bf16<2>(w, scale) : pair_bf16<3>(w, scale);
 }
-__device__ inline void word_pair(uint32_t w, float scale, int i, float &x, float &y) {
-    if (i == 0) pair_f32<0>(w, scale, x, y);
-    else if (i == 1) pair_f32<1>(w, scale, x, y);
-    else if (i == 2) pair_f32<2>(w, scale, x, y);
-    else pair_f32<3>(w, scale, x, y);
-}
 // eight codes
 __device__ inline uint4 word_bf16(uint32_t w, float scale) {
     return make_uint4(pair_bf16<0>(w, scale), pair_bf16<1>(w, scale), pair_bf16<2>(w, scale), pair_bf16<3>(w, scale));

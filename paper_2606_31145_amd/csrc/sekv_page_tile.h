@@ -14,11 +14,11 @@
 
 #include "sekv_page_index.h"
 #include "sekv_page_row.h"
+#include "sekv_page_split.h"
 
 namespace sekv {
 namespace page {
 
-typedef float f4v __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
 
@@ -308,9 +308,10 @@ __device__ inline void put(const PageAttendArgs &a, const Item &it, int chunk, i
 // ------------------------------------------------------------------------------------------
 template <class T, class P, int D>
 struct Keys16 {
-    static constexpr int kBlocks = T::kBytes == 2 ? 2 : 1, kKeys = 16 * kBlocks;
+    static constexpr bool kSplit = T::kBytes == 4 && P::kBytes == 0;          // sekv_page_split.h
+    static constexpr int kBlocks = T::kBytes == 2 || kSplit ? 2 : 1, kKeys = 16 * kBlocks;
     static constexpr int kRow = P::row(D);
-    static constexpr int KW = kRow / 16, VW = kRow >= 64 ? kRow / 64 : 1;     // words a lane
+    static constexpr int KW = kSplit ? 4 : kRow / 16, VW = kRow >= 64 ? kRow / 64 : 1;     // words a lane
     uint32_t k[kBlocks][KW], v[kBlocks][4][VW], ks[kBlocks], vs[kBlocks];
 
     __device__ static size_t base(int row) { return row >= 0 ? row : 0; }     // any row: its keys are masked
@@ -320,6 +321,16 @@ struct Keys16 {
         for (int j = 0; j < kBlocks; ++j) {
             const size_t r0 = base(row[j]);
             const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * kRow;
+            if constexpr (kSplit) {                          // lane g: the row's block g, if it has one
+                uint4 w = make_uint4(0, 0, 0, 0);
+                ks[j] = 127;
+                if (D == 128 || g < P::scales(D)) {
+                    w = *reinterpret_cast<const uint4 *>(kp + m * kRow + 16 * g);
+                    ks[j] = a.k_scale[(r0 + m) * P::scales(D) + g];
+                }
+                k[j][0] = w.x; k[j][1] = w.y; k[j][2] = w.z; k[j][3] = w.w;
+                continue;
+            }
             if constexpr (KW == 2) {
                 const uint2 w = *reinterpret_cast<const uint2 *>(kp + m * kRow + 8 * g);
                 k[j][0] = w.x; k[j][1] = w.y;
@@ -379,9 +390,11 @@ template <class T, class P, int D, int NB>
 struct Rows16 {
     using Tile = Keys16<T, P, D>;
     static constexpr int VE = D / 16, QW = T::kBytes == 2 ? D / 8 : D / 4;    // words of the query a lane
-    static constexpr bool kBf = T::kBytes == 2;
+    static constexpr bool kBf = T::kBytes == 2, kSplit = Tile::kSplit;
     static constexpr int J = Tile::kBlocks;
-    uint32_t q[NB][QW];
+    uint32_t q[NB][kSplit ? 1 : QW];
+    Split32 qs[kSplit ? NB : 1];        // of the lane's block (zeros where a row has no block g)
+    bool odd_scale;                     // a block of queries that does not split
     f4v o[NB][VE];
     float m[NB], l[NB];
     int lo[NB], hi[NB];                 // keys that the column's query sees
@@ -392,6 +405,7 @@ struct Rows16 {
         const int n = lane & 15, gq = lane >> 4, gs = a.group_shift;
         const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
         using E = typename T::elem;
+        odd_scale = false;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             int row = row0 + 16 * nb + n;
@@ -402,8 +416,18 @@ struct Rows16 {
             hi[nb] = int(p < 0 ? -1 : p < cap ? p : cap - 1);
             const E *src = static_cast<const E *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
                            ((g << gs) + (row & ((1 << gs) - 1))) * D;
+            if constexpr (kSplit) {
+                typename Split32::f16v even, odd;
 #pragma unroll
-            for (int i = 0; i < QW / 4; ++i) {
+                for (int i = 0; i < 8; ++i) {
+                    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (D == 128 || gq < P::scales(D)) w = reinterpret_cast<const float4 *>(src + 32 * gq)[i];
+                    even[2 * i] = w.x; odd[2 * i] = w.y; even[2 * i + 1] = w.z; odd[2 * i + 1] = w.w;
+                }
+                odd_scale |= qs[nb].init(even, odd);
+            }
+#pragma unroll
+            for (int i = 0; i < (kSplit ? 0 : QW / 4); ++i) {
                 // the dims of product i: as Keys16 lays out its pieces
                 const int whole = !kBf ? 64 * (i >> 2) + 16 * gq + 4 * (i & 3)
                               : P::kBytes == 2 ? 32 * i + 8 * gq : 64 * (i >> 1) + 16 * gq + 8 * (i & 1);
@@ -413,9 +437,11 @@ struct Rows16 {
             }
             m[nb] = -INFINITY;
             l[nb] = 0.f;
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < VE; ++e) o[nb][e] = f4v{0.f, 0.f, 0.f, 0.f};
-        }
         const int last = row0 + 16 * NB - 1 < it.rows ? row0 + 16 * NB - 1 : it.rows - 1;
         const int64_t p_first = it.p0 + (row0 >> gs), p_last = it.p0 + (last >> gs);
         const int64_t b = p_last - (int64_t(a.window) - 1);
@@ -444,7 +470,10 @@ struct Rows16 {
         for (int j = 0; j < Tile::kBlocks; ++j) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) s[j][nb] = f4v{0.f, 0.f, 0.f, 0.f};
-            if constexpr (kBf) {
+            if constexpr (kSplit) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[j][nb] = mma_split(t.k[j], t.ks[j], qs[nb], s[j][nb]);
+            } else if constexpr (kBf) {
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
                     const uint4 kf = k_frag(t, j, i);
@@ -465,10 +494,6 @@ struct Rows16 {
                     if constexpr (P::kBytes == 4) {
 #pragma unroll
                         for (int u = 0; u < 4; ++u) kf[u] = __uint_as_float(t.k[j][4 * i + u]);
-                    } else if constexpr (P::kBytes == 0) {
-                        const uint32_t w = t.k[j][i >> 1] >> (16 * (i & 1));
-                        pair_f32<0>(w, pow2_of(t.ks[j]), kf[0], kf[1]);
-                        pair_f32<1>(w, pow2_of(t.ks[j]), kf[2], kf[3]);
                     } else {
                         codes4_up(t.k[j][i], pow2_of(t.ks[j]), kf);
                     }
@@ -577,12 +602,19 @@ struct Rows16 {
                     *bad |= wrong != 0;
                 }
         }
-        if constexpr (kBf) {
-            uint4 pf[NB];
+        if constexpr (kBf || kSplit) {
+            constexpr int kParts = kSplit ? 3 : 1;
+            uint4 pf[kParts][NB];
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-                pf[nb] = make_uint4(bf16_pack(s[0][nb][0], s[0][nb][1]), bf16_pack(s[0][nb][2], s[0][nb][3]),
-                                    bf16_pack(s[J - 1][nb][0], s[J - 1][nb][1]), bf16_pack(s[J - 1][nb][2], s[J - 1][nb][3]));
+            for (int nb = 0; nb < NB; ++nb) {
+                float w[8] = {s[0][nb][0], s[0][nb][1], s[0][nb][2], s[0][nb][3],
+                              s[J - 1][nb][0], s[J - 1][nb][1], s[J - 1][nb][2], s[J - 1][nb][3]};
+#pragma unroll
+                for (int p = 0; p < kParts; ++p) {
+                    if constexpr (kSplit) pf[p][nb] = make_uint4(take_bf16(w[0], w[1]), take_bf16(w[2], w[3]), take_bf16(w[4], w[5]), take_bf16(w[6], w[7]));
+                    else pf[p][nb] = make_uint4(bf16_pack(w[0], w[1]), bf16_pack(w[2], w[3]), bf16_pack(w[4], w[5]), bf16_pack(w[6], w[7]));
+                }
+            }
 #pragma unroll
             for (int w = 0; w < VE / 2; ++w) {
                 uint32_t x[J][4];                             // elements 2 w and 2 w + 1 of the lane's rows
@@ -601,7 +633,9 @@ struct Rows16 {
                                                 __builtin_amdgcn_perm(x[J - 1][1], x[J - 1][0], sel),
                                                 __builtin_amdgcn_perm(x[J - 1][3], x[J - 1][2], sel));
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) o[nb][2 * w + u] = mma16(vf, pf[nb], o[nb][2 * w + u]);
+                    for (int p = kParts - 1; p >= 0; --p)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) o[nb][2 * w + u] = mma16(vf, pf[p][nb], o[nb][2 * w + u]);
                 }
             }
         } else {
@@ -611,9 +645,6 @@ struct Rows16 {
                 if constexpr (P::kBytes == 4) {
 #pragma unroll
                     for (int e = 0; e < VE; ++e) vf[e] = __uint_as_float(t.v[0][i][e]);
-                } else if constexpr (P::kBytes == 0) {
-#pragma unroll
-                    for (int w = 0; w < VE / 2; ++w) word_pair(t.v[0][i][0], pow2_of(vs[0][i]), w, vf[2 * w], vf[2 * w + 1]);
                 } else {
 #pragma unroll
                     for (int w = 0; w < VE / 4; ++w) {
@@ -636,8 +667,9 @@ struct Rows16 {
     // ahead; its row blocks one group before that.  Two groups where they fit: 32 ragged sequences in bfloat16 462 us
     // against 469 with one, 4 of 131072 in 8 bits 188.6 against 191.2, 13 of float and head_dim 64 577 against 599.
     // In 4 bits three: 32 ragged sequences 168.7 us against 173.4 with two, 167.8 with four, 4 of 131072 109.9, 109.5, 110.6.
-    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 2 : 0)), kHeld = NB * (D / 4 + QW);
-    static constexpr int kAhead = P::kBytes == 0 ? 3 : 2 * kTileWords + kHeld <= 176 ? 2 : 1;     // of 256 registers
+    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 2 : 0)), kHeld = NB * (D / 4 + (kSplit ? 6 * kPieces + 2 : QW));
+    static constexpr int kRoom = kSplit ? 150 : 176;                          // of 256 registers
+    static constexpr int kAhead = P::kBytes == 0 && 3 * kTileWords + kHeld <= kRoom ? 3 : 2 * kTileWords + kHeld <= kRoom ? 2 : 1;
     __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int step, bool *bad, int lane) {
         if (pos >= it.end) return;
         Tile t[kAhead];
