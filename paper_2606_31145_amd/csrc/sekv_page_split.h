@@ -4,8 +4,8 @@
 // lane, at 59 times the rate of the float one (9.05 PFLOP/s and 154 TFLOP/s measured), and its products and sums are
 // exact to float's last bit: both factors are small whole numbers times a power of two.  So a query's block of 32 floats
 // is written as a sum of six 6-bit numbers (sign, 2 bits of exponent, 3 of mantissa, largest 7.5), each piece rounded
-// from what the last one left and 2^-4 of its scale.  After six, what is left is below 2^-25 of the block's largest
-// value, half a step of it as a float.
+// from what the last one left and 2^-4 of its scale.  After six, what is left is below 2^-24 of the block's largest
+// value: a rounding of that one, and for smaller values of the block a coarser one than their own.
 //
 // Values.  A 4-bit code with its scale is a bfloat16 number; a float weight is the sum of three, to 2^-25 of it.
 #pragma once
@@ -19,7 +19,8 @@ constexpr int kPieces = 6;
 typedef uint32_t u6v __attribute__((ext_vector_type(6)));
 
 // Values 2 i and 2 i + 1 of a block in even and odd.  True where the scales of the later pieces would end below a
-// float's exponents: such a block's products are left to plain arithmetic.
+// float's exponents, and where a value is infinite, whose products have a sign: such a block's products are left to
+// plain arithmetic.  NaN makes every product NaN.
 struct Split32 {
     u6v piece[kPieces];
     uint32_t scale[2];                                       // exponent bytes, four a word
@@ -55,7 +56,7 @@ struct Split32 {
                 odd[i] -= back[2 * i + 1];
             }
         }
-        return small && top != 0;
+        return (small && top != 0) || top == 0x7f800000u;
     }
 };
 

@@ -304,6 +304,94 @@ def test_nan_blocks_reach_those_who_see_them(S, dtype, news, group, dim, window)
                 assert ((lse[i].double() - rl[i]).abs() <= ltol[i]).all(), (which, b, t, i)
 
 
+def _two(n):
+    return torch.exp2(n.double())
+
+
+QUERIES = {                                              # factors of the queries [tokens][heads][dim], of the keys' exponents
+    "one large value": (lambda x, g: x * torch.where(torch.arange(x.shape[-1]) == 5, 1000.0, 1.0), 0),
+    "many sizes": (lambda x, g: x * _two(torch.randint(-14, 3, x.shape, generator=g)), 0),
+    "one size a block": (lambda x, g: x * _two(torch.randint(-30, 3, x.shape[:-1] + (x.shape[-1] // 32, 1), generator=g)
+                                               .expand(*x.shape[:-1], x.shape[-1] // 32, 32).flatten(-2)), 0),
+    "tiny": (lambda x, g: x * 2.0 ** -100, 100),
+    "some rows tiny": (lambda x, g: x * _two(-110 * torch.randint(0, 2, x.shape[:2] + (1,), generator=g)), 0),
+    "huge": (lambda x, g: x * 2.0 ** 100, -100),
+    "zeros": (lambda x, g: x * 0.0, 0),
+    "zeros in blocks": (lambda x, g: x * (torch.arange(x.shape[-1]) >= 32), 0),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news,group,dim", SHAPES)
+@pytest.mark.parametrize("kind", list(QUERIES))
+def test_queries_of_all_sizes(S, dtype, news, group, dim, kind):
+    """Float queries are written as six pieces of a block of 32, each off by half a step of the last: what is left of a
+    value is below 2^-24 of the block's largest, and a score off by that times the block's keys besides the case's bound.
+    That bound takes roundings as relative; a weight, or its product with a value, that falls below 2^-126 has no bits
+    there and is off by up to 2^-126 itself: over n keys 2^-126 (n + sum |v|)."""
+    banner(f"queries {kind} {dtype} {news} {group} {dim}")
+    c = Case4(dtype, [200, 77] + [0] * (len(news) - 2), news, group=group, dim=dim, page=32, seed=_seed(kind, news, dim))
+    make, up = QUERIES[kind]
+    c.q = make(c.q.double(), torch.Generator().manual_seed(7)).to(TORCH[dtype])
+    if up:
+        c.codes["k"][1].copy_((c.codes["k"][1].int() + up).clamp(2, 252).to(torch.uint8))
+        c.pools["k"] = decode4(*c.codes["k"])
+    ref, rl, tol, ltol = c.attend()
+    for b, n in enumerate(c.lens):
+        for g in range(c.Hkv if c.news[b] else 0):
+            K = c.dense("k", b, g)[0].abs().unflatten(-1, (-1, 32)).sum(-1).amax(0)
+            V = c.dense("v", b, g)[0].abs()
+            h = slice(g * c.G, (g + 1) * c.G)
+            rows = slice(c.start[b], c.start[b + 1])
+            tol[rows, h] += 2.0 ** -126 * (n + V.sum(0))
+            if dtype == "f32":
+                err = (c.q[rows, h].double().unflatten(-1, (-1, 32)).abs().amax(-1) @ K) * 2.0 ** -24 * c.scale
+                ltol[rows, h] += err
+                tol[rows, h] += 2 * err[..., None] * V.amax(0)
+    out, lse, status = _attend(S, c)
+    ratio, lratio = ((out.double() - ref).abs() / tol).max().item(), ((lse.double() - rl).abs() / ltol).max().item()
+    banner(f"  error / bound: out {ratio:.3f}, lse {lratio:.3f}")
+    assert ratio <= 1.0 and lratio <= 1.0 and status == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news,group,dim", SHAPES)
+def test_queries_of_no_number(S, dtype, news, group, dim):
+    """NaN, and an infinity beside it, in some heads' queries: their results are NaN and all others as without."""
+    banner(f"queries nan {dtype} {news} {group} {dim}")
+    c = Case4(dtype, [200, 77] + [0] * (len(news) - 2), news, group=group, dim=dim, page=32, seed=_seed(news, dim))
+    ref, rl, tol, ltol = c.attend()
+    bad = torch.rand(c.q.shape[:2], generator=torch.Generator().manual_seed(3)) < 0.3
+    bad[0, 0], bad[-1, -1] = True, False
+    c.q[..., 3][bad] = math.nan
+    c.q[..., 40][bad] = -math.inf
+    out, lse, _ = _attend(S, c)
+    assert out[bad].isnan().all() and lse[bad].isnan().all()
+    assert ((out.double() - ref).abs() <= tol)[~bad].all() and ((lse.double() - rl).abs() <= ltol)[~bad].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("news,group,dim", SHAPES)
+def test_infinite_queries(S, dtype, news, group, dim):
+    """Infinities in some heads' queries against keys above 0: all scores -inf give zeros, any of inf no number."""
+    banner(f"queries inf {dtype} {news} {group} {dim}")
+    c = Case4(dtype, [200, 77] + [0] * (len(news) - 2), news, group=group, dim=dim, page=32, seed=_seed(news, dim))
+    codes, E = c.codes["k"]
+    codes[..., 1] = codes[..., 1] & 0x7f | 0x10             # value 3 of a row: positive, not 0
+    c.pools["k"] = decode4(codes, E)
+    ref, rl, tol, ltol = c.attend()
+    pick = torch.rand(c.q.shape[:2], generator=torch.Generator().manual_seed(3))
+    pick[0, 0] = 0.0
+    low, high = pick < 0.2, pick > 0.8
+    c.q[..., 3][low] = -math.inf
+    c.q[..., 3][high] = math.inf
+    out, lse, _ = _attend(S, c)
+    assert not out[low].any() and (lse[low] == -math.inf).all()
+    assert out[high].isnan().all() and not torch.isfinite(lse[high]).any()
+    rest = ~low & ~high
+    assert ((out.double() - ref).abs() <= tol)[rest].all() and ((lse.double() - rl).abs() <= ltol)[rest].all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("news,group,dim", SHAPES)
 def test_scores_past_two_to_the_26(S, dtype, news, group, dim):
