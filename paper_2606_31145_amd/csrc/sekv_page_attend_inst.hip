@@ -44,17 +44,12 @@ __device__ inline bool any_of(bool x, int lane, int wave) {
     else return __syncthreads_or(x);
 }
 
-// At most 16 NB rows: every wave takes all of them, and every fourth step of the keys.  True when the
-// item has to be done again by plain_rows.
+// The four waves' parts of the same rows of an item, joined through LDS.  True when the item has to be done again by
+// plain_rows.
 template <class T, class P, int D, int NB>
-__device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
-    using R = Rows16<T, P, D, NB>;
-    constexpr int VE = R::VE, RS = D + 4, kKeys = R::Tile::kKeys, N = 16 * NB;
-    R r;
-    r.init(a, it, g, 0, lane);
-    bool bad = r.odd_scale;
-    r.run(a, it, b, g, it.begin + wave * kKeys, kKeys * kWaves, &bad, lane);
-    // the four waves' parts, joined through LDS
+__device__ inline bool join_waves(const PageAttendArgs &a, const Item &it, const Rows16<T, P, D, NB> &r, bool bad, int g, int c,
+                                  int lane, int wave, unsigned char *lds) {
+    constexpr int VE = D / 16, RS = D + 4, N = 16 * NB;
     float *ml = reinterpret_cast<float *>(lds), *so = ml + kWaves * 2 * N;
     const int n = lane & 15, gq = lane >> 4;
 #pragma unroll
@@ -95,17 +90,27 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
     return false;
 }
 
-// Up to 128 float rows: 32 to a wave, which reads all the item's keys.
+// At most 16 NB rows: every wave takes all of them, and every fourth step of the keys.
+template <class T, class P, int D, int NB>
+__device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
+    using R = Rows16<T, P, D, NB>;
+    R r;
+    bool bad = false;
+    r.run(a, it, b, g, 0, it.begin + wave * R::Tile::kKeys, R::Tile::kKeys * kWaves, &bad, lane);
+    return join_waves<T, P, D, NB>(a, it, r, bad, g, c, lane, wave, lds);
+}
+
+// Up to 128 float rows: 32 to a wave, which reads all the item's keys.  Over 4-bit pages up to 32 as well, as in narrow:
+// in one piece of code, for with two of them the kernels of a call are past the instruction cache's 64 KB.
 template <class P, int D>
-__device__ inline bool wide_f32(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave) {
+__device__ inline bool float_rows(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
     using R = Rows16<F32, P, D, 2>;
     R r;
     bool bad = false;
-    if (wave * 32 < it.rows) {
-        r.init(a, it, g, wave * 32, lane);
-        bad = r.odd_scale;
-        r.run(a, it, b, g, it.begin, R::Tile::kKeys, &bad, lane);
-    }
+    const bool few = P::kBytes == 0 && it.narrow;
+    const int row0 = few ? 0 : wave * 32, at = few ? wave : 0, of = few ? kWaves : 1;
+    if (row0 < it.rows) r.run(a, it, b, g, row0, it.begin + at * R::Tile::kKeys, of * R::Tile::kKeys, &bad, lane);
+    if (few) return join_waves<F32, P, D, 2>(a, it, r, bad, g, c, lane, wave, lds);
     if (any_of<P>(bad, lane, wave)) return true;
     if (wave * 32 >= it.rows) return false;
     const int n = lane & 15, gq = lane >> 4;
@@ -252,9 +257,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
     if (!plan.chunk || !find_item(a, x, lane, plan, lds, &b, &c, &it)) return;
     bool again;
     if (it.narrow && it.rows <= 16) again = narrow<T, P, D, 1>(a, it, b, g, c, lane, wave, lds);
-    else if (it.narrow) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);
+    else if (it.narrow && (T::kBytes == 2 || P::kBytes != 0)) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);
     else if constexpr (T::kBytes == 2) again = wide_bf16<P, D>(a, it, b, g, c, lane, wave, lds);
-    else again = wide_f32<P, D>(a, it, b, g, c, lane, wave);
+    else again = float_rows<P, D>(a, it, b, g, c, lane, wave, lds);
     if (again) plain_rows<T, P, D>(a, it, b, g, c, lane, wave);
     if (it.chunk0 == it.chunk1 || a.join_launch) return;
     // the last of a tile's workgroups joins their partials: all stores of this one have to be out before it

@@ -670,11 +670,11 @@ struct Rows16 {
     static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 2 : 0)), kHeld = NB * (D / 4 + (kSplit ? 6 * kPieces + 2 : QW));
     static constexpr int kRoom = kSplit ? 150 : 176;                          // of 256 registers
     static constexpr int kAhead = P::kBytes == 0 && 3 * kTileWords + kHeld <= kRoom ? 3 : 2 * kTileWords + kHeld <= kRoom ? 2 : 1;
-    __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int pos, int step, bool *bad, int lane) {
-        if (pos >= it.end) return;
+    __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int row0, int pos, int step, bool *bad, int lane) {
         Tile t[kAhead];
         uint32_t valid[kAhead];
         int row[J];
+        if constexpr (!kSplit) init(a, it, g, row0, lane);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             look(a, it, b, g, pos + u * step, row, lane);
@@ -684,6 +684,11 @@ struct Rows16 {
                 t[u].load_values(a, row, lane);
             }
         }
+        if constexpr (kSplit) {                               // splitting the queries takes a while: the keys come meanwhile
+            init(a, it, g, row0, lane);
+            *bad |= odd_scale;
+        }
+        if (pos >= it.end) return;
         for (;;) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
