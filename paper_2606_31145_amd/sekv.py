@@ -788,9 +788,14 @@ class PageCache:
         """The C view.  Types, sizes and devices are checked against pd when an attribute was set, a
         tensor has moved or pd is another than in the last call.  A tensor's shape and strides are not to
         be changed in place meanwhile: set the attribute instead."""
-        seen = (bytes(pd), *[None if x is None else x.data_ptr() for x in self._tensors()])
-        if seen == self._seen:
-            return self._struct
+        ks, vs = self.k_scale, self.v_scale
+        try:
+            seen = (bytes(pd), self.k_pages.data_ptr(), self.v_pages.data_ptr(), None if ks is None else ks.data_ptr(),
+                    None if vs is None else vs.data_ptr(), self.page_table.data_ptr(), self.seq_len.data_ptr())
+            if seen == self._seen:
+                return self._struct
+        except AttributeError:                               # something is no tensor, which the checks say
+            seen = None
         pool, scales = _page_shapes(pd)
         want = _PAGE_STORAGE[pd.page_dtype] if pd.page_dtype in _PAGE_STORAGE else None
         dev = self.k_pages.device
@@ -823,13 +828,16 @@ def _token_rows(pd: PageDims, x, name, heads, device):
 
 def _rows_of(dtype, d, x, name, heads, device):
     """(n_tokens, address, token stride)"""
-    n = x.shape[0]
-    if x.dtype is not dtype or x.shape != (n, heads, d) or x.device != device:
-        _expect(x, name, dtype, (n, heads, d), device)
-    s = x.stride()
-    if n and (s[2] != 1 or (heads > 1 and s[1] != d)):
+    try:
+        n, h, w = x.shape
+        step, row, one = x.stride()
+    except (AttributeError, ValueError):                     # no tensor, or another number of dimensions
+        n = h = w = None
+    if h != heads or w != d or x.dtype is not dtype or x.device != device:
+        _expect(x, name, dtype, ("n_tokens" if n is None else n, heads, d), device)
+    if n and (one != 1 or (heads > 1 and row != d)):
         raise ValueError(f"{name}: a token's heads have to lie one after another")
-    return n, x.data_ptr(), s[0] if n > 1 else heads * d
+    return n, x.data_ptr(), step if n > 1 else heads * d
 
 
 def _tok_start(pd: PageDims, tok_start, device):
@@ -840,7 +848,9 @@ def _ints(x, name, n, device):
     """Address of an int32 [n] tensor."""
     if not isinstance(x, torch.Tensor) or x.dtype is not torch.int32 or x.shape != (n,) or x.device != device:
         _expect(x, name, torch.int32, (n,), device)
-    return _ptr(x)
+    if not x.is_contiguous():
+        raise ValueError("tensors passed to the library must be contiguous")
+    return x.data_ptr()
 
 
 _HERE = contextlib.nullcontext()
@@ -852,8 +862,8 @@ def _on(device, stream, what="pages"):
     if device.type != "cuda":
         raise ValueError(f"the {what} have to be on a GPU")
     if stream is None:
-        st = torch._C._cuda_getCurrentRawStream(device.index)
-        return _HERE if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device), st
+        at, C = device.index, torch._C
+        return _HERE if at == C._cuda_getDevice() else torch.cuda.device(device), C._cuda_getCurrentRawStream(at)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     if stream.device != device:
@@ -903,16 +913,21 @@ class Rotary:
     def __init__(self, freq, layout: str = "half", scale: float = 1.0):
         if not isinstance(freq, torch.Tensor) or freq.dtype != torch.float64 or freq.dim() != 1:
             raise ValueError("freq: a float64 tensor [rot_dim / 2]")
-        self.freq = freq.contiguous()
-        self._struct = RotaryStruct(2 * len(freq), _ROTARY_LAYOUTS[layout], self.freq.data_ptr(), float(scale))
+        self._freq = freq.contiguous()
+        self._device = self._freq.device
+        self._struct = RotaryStruct(2 * len(freq), _ROTARY_LAYOUTS[layout], self._freq.data_ptr(), float(scale))
+
+    @property
+    def freq(self):
+        return self._freq
 
     @property
     def rot_dim(self) -> int:
         return self._struct.rot_dim
 
     def struct(self, device) -> RotaryStruct:
-        if self.freq.device != device:
-            raise ValueError(f"the frequencies are on {self.freq.device}, the rows on {device}")
+        if self._device != device:
+            raise ValueError(f"the frequencies are on {self._device}, the rows on {device}")
         return self._struct
 
 
