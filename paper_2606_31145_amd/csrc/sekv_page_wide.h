@@ -124,15 +124,25 @@ struct Stage<E2M1, D> {
         vs = keep ? vs : 127u;
         return vs >= kOverExponent4;
     }
+    // The value pieces of a lane in an order that differs by its row: in the same order the four rows of 16 lanes, whose
+    // pieces lie 64 bytes apart on purpose (Swizzle), would be in the same banks.
     __device__ void store(unsigned char *kt, unsigned char *vt, int row0, int lane) const {
         using Z = Swizzle<D>;
-        const int row = row0 + lane / 4, c = lane % 4 * W;
+        const int row = row0 + lane / 4, c = lane % 4 * W, turn = D == 128 ? row & 3 : (row >> 1) & 1;
         unsigned char *kr = kt + row * (D * 2), *vr = vt + row * (D * 2);
         const float fk = pow2_of(ks), fv = pow2_of(vs);
+        wv x;
+#pragma unroll
+        for (int u = 0; u < W; ++u) x[u] = turn & 1 ? v[u ^ 1] : v[u];
+        if constexpr (W == 4) {
+            const wv y = x;
+#pragma unroll
+            for (int u = 0; u < W; ++u) x[u] = turn & 2 ? y[u ^ 2] : y[u];
+        }
 #pragma unroll
         for (int u = 0; u < W; ++u) {
             *reinterpret_cast<uint4 *>(kr + (((c + u) ^ Z::key(row)) << 4)) = word_bf16(k[u], fk);
-            *reinterpret_cast<uint4 *>(vr + (((c + u) ^ Z::value(row)) << 4)) = word_bf16(v[u], fv);
+            *reinterpret_cast<uint4 *>(vr + (((c + (u ^ turn)) ^ Z::value(row)) << 4)) = word_bf16(x[u], fv);
         }
     }
 };
