@@ -124,25 +124,31 @@ struct Stage<E2M1, D> {
         vs = keep ? vs : 127u;
         return vs >= kOverExponent4;
     }
-    // The value pieces of a lane in an order that differs by its row: in the same order the four rows of 16 lanes, whose
-    // pieces lie 64 bytes apart on purpose (Swizzle), would be in the same banks.
+    // Eight lanes, of two rows, write at a time, 16 bytes each, and the 128 bytes that they fill should not share banks.
+    // So a lane takes its pieces in an order of its own: number u ^ turn in step u.  All in the order of u, with two lanes
+    // (keys) or four (values) in the same banks, 2048 tokens over 32768 take 1121 us instead of 1097.
+    __device__ static wv turned(wv x, int turn) {
+        wv y;
+#pragma unroll
+        for (int u = 0; u < W; ++u) y[u] = turn & 1 ? x[u ^ 1] : x[u];
+        if constexpr (W == 4) {
+            x = y;
+#pragma unroll
+            for (int u = 0; u < W; ++u) y[u] = turn & 2 ? x[u ^ 2] : x[u];
+        }
+        return y;
+    }
     __device__ void store(unsigned char *kt, unsigned char *vt, int row0, int lane) const {
         using Z = Swizzle<D>;
-        const int row = row0 + lane / 4, c = lane % 4 * W, turn = D == 128 ? row & 3 : (row >> 1) & 1;
+        const int row = row0 + lane / 4, c = lane % 4 * W;
+        const int second = lane >> 2 & 1, turn_k = D == 128 ? lane & 2 : second, turn_v = D == 128 ? turn_k | second : second;
         unsigned char *kr = kt + row * (D * 2), *vr = vt + row * (D * 2);
         const float fk = pow2_of(ks), fv = pow2_of(vs);
-        wv x;
-#pragma unroll
-        for (int u = 0; u < W; ++u) x[u] = turn & 1 ? v[u ^ 1] : v[u];
-        if constexpr (W == 4) {
-            const wv y = x;
-#pragma unroll
-            for (int u = 0; u < W; ++u) x[u] = turn & 2 ? y[u ^ 2] : y[u];
-        }
+        const wv kx = turned(k, turn_k), vx = turned(v, turn_v);
 #pragma unroll
         for (int u = 0; u < W; ++u) {
-            *reinterpret_cast<uint4 *>(kr + (((c + u) ^ Z::key(row)) << 4)) = word_bf16(k[u], fk);
-            *reinterpret_cast<uint4 *>(vr + (((c + (u ^ turn)) ^ Z::value(row)) << 4)) = word_bf16(x[u], fv);
+            *reinterpret_cast<uint4 *>(kr + (((c + (u ^ turn_k)) ^ Z::key(row)) << 4)) = word_bf16(kx[u], fk);
+            *reinterpret_cast<uint4 *>(vr + (((c + (u ^ turn_v)) ^ Z::value(row)) << 4)) = word_bf16(vx[u], fv);
         }
     }
 };
