@@ -6,11 +6,12 @@
 // cost it about 4 vector instructions and one exponential each for 64 lanes, so the two units are about
 // equally busy and two workgroups share a compute unit to keep both fed.  Keys and values are fetched
 // once per workgroup (each wave one block of 16 keys, which lies in one page), a tile ahead: bfloat16
-// straight into LDS, 8-bit codes through registers, where they become scaled bfloat16, so that the rest
+// straight into LDS, codes of 8 and 4 bits through registers, where they become scaled bfloat16, so that the rest
 // knows one type only.
 //
 // Measured, 2048 tokens over 32768 keys, head_dim 128, bfloat16 (1065 GFLOP): 1060 to 1150 us by the card, 925 to
-// 1005 TFLOP/s, where a 16384^3 matrix product reaches 1364; in 8 bits 1081 us; head_dim 64 665 us.
+// 1005 TFLOP/s, where a 16384^3 matrix product reaches 1364; in 8 bits 1081 us, in 4 bits 1063 to 1097;
+// head_dim 64 665 us.
 // The matrix cores are busy for 48 % of the cycles, at a clock that the load brings down to 1.95 GHz.
 // The way there: 1211 us with the blocks of a tile looked up by one lane each instead of by all, 1166; the LDS reads placed among the products
 // (sched_group_barrier) 1146; bfloat16 straight into LDS 1067.  No gain came from a priority for half of

@@ -169,6 +169,8 @@ def test_binding_checks_tensors(S):
     pd, cache, ts = c.dims(S), c.cache(S, "cpu"), c.tok_start("cpu")
     r, pos = S.Rotary(frequencies(64)), torch.arange(4, dtype=torch.int32)
     assert r.rot_dim == 64
+    with pytest.raises(AttributeError):
+        r.freq = frequencies(64)                         # the C view holds the address of the one it was made of
     for bad in (frequencies(64).float(), frequencies(64)[None], [1.0]):
         with pytest.raises(ValueError, match="freq"):
             S.Rotary(bad)
@@ -196,3 +198,12 @@ def test_binding_checks_tensors(S):
         a.update(kw)
         with pytest.raises(ValueError, match=match):
             S.page_append_rotary(pd, cache, r, ws=None, **a)
+    for name in "qkv":                                   # no tensor, and one of other dimensions
+        for bad, error in ((getattr(c, name).tolist(), TypeError), (getattr(c, name)[0], ValueError)):
+            a = dict(q=c.q, k=c.k, v=c.v, tok_start=ts)
+            a[name] = bad
+            with pytest.raises(error, match=f"{name}:"):
+                S.page_append_rotary(pd, cache, r, ws=None, **a)
+    cache.page_table = None
+    with pytest.raises(TypeError, match="page_table"):
+        S.page_append_rotary(pd, cache, r, c.q, c.k, c.v, ts, None)
