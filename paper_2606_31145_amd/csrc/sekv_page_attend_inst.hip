@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
     int b = 0, c = 0, g = 0;
     const uint32_t x = place_of(blockIdx.x, a.t.Hkv, &g);
     Item it;
-    if (!plan.chunk || !find_item(a, x, lane, plan, lds, &b, &c, &it)) return;
+    if (!plan.chunk || !find_item<false, P::kBytes == 0>(a, x, lane, plan, lds, &b, &c, &it)) return;
     bool again;
     if (it.narrow && it.rows <= 16) again = narrow<T, P, D, 1>(a, it, b, g, c, lane, wave, lds);
     else if (it.narrow && (T::kBytes == 2 || P::kBytes != 0)) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);

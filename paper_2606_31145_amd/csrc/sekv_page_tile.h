@@ -159,7 +159,9 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, bool fo
 // Pair x of the call: sequences in order, chunks of a sequence in order, tiles last first (the later
 // tokens of a chunk see more keys).  kTiles: tile x instead, as its first chunk's item.  x and so the result are
 // the same in all threads.  lds as above.
-template <bool kTiles = false>
+// kWideFirst: of up to 64 sequences those of wide tiles come first, whose items last longest: they start on compute units
+// of their own, and the short ones join them.  KEEPFIG
+template <bool kTiles = false, bool kWideFirst = false>
 __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, const Plan &p, unsigned char *lds, int *b_out,
                                  int *c_out, Item *it) {
     const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
@@ -172,6 +174,16 @@ __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, 
         for (int b = b0; b < b1; ++b) n += pairs(load_seq(a, b));
     } else if (lane < a.t.B) {
         n = pairs(p.mine);
+    }
+    int whose = lane;                                        // the sequence whose pairs are counted at this place
+    if constexpr (kWideFirst) {
+        const unsigned long long wide = __ballot(!many && lane < a.t.B && (p.mine.nq << a.group_shift) > kFewRows);
+        if (wide) {
+            const unsigned long long before = (1ull << lane) - 1;
+            const int to = wide >> lane & 1 ? __popcll(wide & before) : __popcll(wide) + __popcll(~wide & before);
+            n = __builtin_amdgcn_ds_permute(to << 2, n);
+            whose = __builtin_amdgcn_ds_permute(to << 2, lane);
+        }
     }
     uint32_t incl = n;
     if (a.t.B > 1) {
@@ -215,8 +227,9 @@ __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, 
         if (!past) return false;
         const int l = __ffsll(past) - 1;
         in = x - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l));
-        s = of_lane(p.mine, l);
-        *b_out = l;
+        const int b = __builtin_amdgcn_readlane(whose, l);
+        s = of_lane(p.mine, b);
+        *b_out = b;
     }
     *c_out = int(in / uint32_t(s.tiles));
     *it = make_item(s, s.tiles - 1 - int(in % uint32_t(s.tiles)), *c_out, p.chunk, cap, a.window, a.group_shift);
