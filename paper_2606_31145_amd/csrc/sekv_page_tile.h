@@ -160,7 +160,9 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, bool fo
 // tokens of a chunk see more keys).  kTiles: tile x instead, as its first chunk's item.  x and so the result are
 // the same in all threads.  lds as above.
 // kWideFirst: of up to 64 sequences those of wide tiles come first, whose items last longest: they start on compute units
-// of their own, and the short ones join them.  KEEPFIG
+// of their own, and the short ones join them.  Over 4-bit pages (us): 7 ragged sequences, two of them chunks, in float 38.8
+// in order and 32.8 so, 13 of which one has 257 tokens 141 and 131, 32 of up to 2000 100 and 85; with no wide tile 8.9 and 9.0.
+// In 8 bits 13 sequences 90.4 and 90.6: there the order stays.
 template <bool kTiles = false, bool kWideFirst = false>
 __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, const Plan &p, unsigned char *lds, int *b_out,
                                  int *c_out, Item *it) {

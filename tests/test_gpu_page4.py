@@ -215,6 +215,10 @@ ATTENDS = [
     dict(lens=[700] + [20] * 39, news=[40] + [0] * 39, group=4, dim=128, page=32),
     dict(lens=[700, 90] + [20] * 58, news=[40, 17] + [0] * 57 + [1], group=8, kv_heads=1, dim=64, page=16, window=300),
     dict(lens=[60, 900] + [0] * 9, news=[5, 6] + [0] * 9, group=8, kv_heads=3, dim=128, page=16),
+    # wide tiles behind narrow ones and none: of 64 sequences they start first, of 65 in order
+    dict(lens=[50] * 40 + [700] + [0] * 20 + [400, 30, 600], news=[1] * 40 + [100] + [0] * 20 + [40, 1, 150], kv_heads=3, dim=128),
+    dict(lens=[50] * 40 + [700] + [0] * 21 + [400, 30, 600], news=[1] * 40 + [100] + [0] * 21 + [40, 1, 150], kv_heads=3, dim=64),
+    dict(lens=[900, 800, 1000], news=[1, 0, 333], kv_heads=4, group=2, dim=64, window=300),
 ]
 
 
