@@ -45,6 +45,14 @@ __device__ inline bool any_of(bool x, int lane, int wave) {
     else return __syncthreads_or(x);
 }
 
+// LDS of a workgroup's 16 NB rows: four waves' maxima and sums, then each wave's rows, where its queries pass before: what a
+// wave writes early reaches no other's.
+template <int D, int NB> constexpr int kRowBytes = 16 * NB * (D + 4) * 4;
+template <int D, int NB>
+__device__ inline unsigned char *own_rows(unsigned char *lds, int wave) {
+    return lds + kWaves * 2 * 16 * NB * 4 + wave * kRowBytes<D, NB>;
+}
+
 // The four waves' parts of the same rows of an item, joined through LDS.  True when the item has to be done again by
 // plain_rows.
 template <class T, class P, int D, int NB>
@@ -97,7 +105,7 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
     using R = Rows16<T, P, D, NB>;
     R r;
     bool bad = false;
-    r.run(a, it, b, g, 0, it.begin + wave * R::Tile::kKeys, R::Tile::kKeys * kWaves, &bad, lane);
+    r.run(a, it, b, g, 0, it.begin + wave * R::Tile::kKeys, R::Tile::kKeys * kWaves, &bad, lane, own_rows<D, NB>(lds, wave));
     return join_waves<T, P, D, NB>(a, it, r, bad, g, c, lane, wave, lds);
 }
 
@@ -111,11 +119,38 @@ __device__ inline bool float_rows(const PageAttendArgs &a, const Item &it, int b
     bool bad = false;
     const bool few = P::kBytes == 0 && it.narrow;
     const int row0 = few ? 0 : wave * 32, at = few ? wave : 0, of = few ? kWaves : 1;
-    if (row0 < it.rows) r.run(a, it, b, g, row0, it.begin + at * R::Tile::kKeys, of * R::Tile::kKeys, &bad, lane);
+    if (row0 < it.rows) r.run(a, it, b, g, row0, it.begin + at * R::Tile::kKeys, of * R::Tile::kKeys, &bad, lane, own_rows<D, 2>(lds, wave));
     if (few) return join_waves<F32, P, D, 2>(a, it, r, bad, g, c, lane, wave, lds);
     if (any_of<P>(bad, lane, wave)) return true;
     if (wave * 32 >= it.rows) return false;
     const int n = lane & 15, gq = lane >> 4;
+    if constexpr (P::kBytes == 0) {
+        // through LDS, so that a store covers whole rows: straight from the registers it touches 64 of them
+        constexpr int RS = D + 4, GT = D / 4;
+        float *so = reinterpret_cast<float *>(own_rows<D, 2>(lds, wave));
+        float m[2], l[2];
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+            m[nb] = r.m[nb];
+            l[nb] = r.sum(nb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < R::VE; ++e) so[(16 * nb + n) * RS + R::VE * (4 * gq + i) + e] = r.o[nb][e][i];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r0 = 0; r0 < 32; r0 += 64 / GT) {
+            const int row = r0 + lane / GT, rw = wave * 32 + row, d0 = lane % GT * 4;
+            const float4 x = *reinterpret_cast<const float4 *>(so + row * RS + d0);
+            const float o[4] = {x.x, x.y, x.z, x.w};
+            const float mr = __shfl(r0 < 16 ? m[0] : m[1], row & 15), lr = __shfl(r0 < 16 ? l[0] : l[1], row & 15);
+            if (rw < it.rows)
+                put<F32, D>(a, it, c, it.tok0 + (rw >> a.group_shift), (g << a.group_shift) + (rw & ((1 << a.group_shift) - 1)),
+                            d0, o, mr, lr);
+        }
+        return false;
+    }
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb) {
         const int rw = wave * 32 + nb * 16 + n;

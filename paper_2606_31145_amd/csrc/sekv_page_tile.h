@@ -416,7 +416,8 @@ struct Rows16 {
     int lo_all, hi_all, lo_any, hi_any; // keys that every column sees, that some column sees
 
     // Columns: rows row0 + 16 nb + lane % 16 of the item.
-    __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane) {
+    // lds: the wave's own, for 16 rows of floats (two tiles, split queries).
+    __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane, unsigned char *lds) {
         const int n = lane & 15, gq = lane >> 4, gs = a.group_shift;
         const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
         using E = typename T::elem;
@@ -432,11 +433,38 @@ struct Rows16 {
             const E *src = static_cast<const E *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
                            ((g << gs) + (row & ((1 << gs) - 1))) * D;
             if constexpr (kSplit) {
+                // Two tiles of rows: a load covers whole rows, and LDS hands each lane its block; straight into the lanes it
+                // would touch 64 lines at a time, eight times over.  With the stores of float_rows the same way: 16 float
+                // sequences of 900 keys, chunks of up to 100 tokens beside single ones, 60.0 us and 49.3, 257 tokens over
+                // 9001 115.8 and 113.4.  With one tile the rows are mostly fewer: one token of 32 sequences of up to 9000
+                // straight 65.2, through LDS 66.0.  Pieces of 16 bytes sit at their index XOR the row's, for the banks.
+                if constexpr (NB == 2) {
+                    constexpr int L = D / 4;                  // pieces, and lanes, of a row
+                    typedef uint32_t w4v __attribute__((ext_vector_type(4)));
+                    w4v w[16 * L / 64];
+#pragma unroll
+                    for (int i = 0; i < 16 * L / 64; ++i) {
+                        int at = row0 + 16 * nb + i * (64 / L) + lane / L;
+                        at = at < it.rows ? at : it.rows - 1;
+                        w[i] = reinterpret_cast<const w4v *>(static_cast<const E *>(a.q) + int64_t(it.tok0 + (at >> gs)) * a.q_stride +
+                                                             ((g << gs) + (at & ((1 << gs) - 1))) * D)[lane % L];
+                    }
+                    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                    for (int i = 0; i < 16 * L / 64; ++i) {
+                        const int at = i * (64 / L) + lane / L;
+                        *reinterpret_cast<w4v *>(lds + at * (D * 4) + ((lane % L ^ (at & 7)) << 4)) = w[i];
+                    }
+                    __builtin_amdgcn_wave_barrier();
+                }
                 typename Split32::f16v even, odd;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (D == 128 || gq < P::scales(D)) w = reinterpret_cast<const float4 *>(src + 32 * gq)[i];
+                    if (D == 128 || gq < P::scales(D)) {
+                        if constexpr (NB == 2) w = *reinterpret_cast<const float4 *>(lds + n * (D * 4) + (((8 * gq + i) ^ (n & 7)) << 4));
+                        else w = reinterpret_cast<const float4 *>(src + 32 * gq)[i];
+                    }
                     even[2 * i] = w.x; odd[2 * i] = w.y; even[2 * i + 1] = w.z; odd[2 * i + 1] = w.w;
                 }
                 odd_scale |= qs[nb].init(even, odd);
@@ -685,11 +713,12 @@ struct Rows16 {
     static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 2 : 0)), kHeld = NB * (D / 4 + (kSplit ? 6 * kPieces + 2 : QW));
     static constexpr int kRoom = kSplit ? 150 : 176;                          // of 256 registers
     static constexpr int kAhead = P::kBytes == 0 && 3 * kTileWords + kHeld <= kRoom ? 3 : 2 * kTileWords + kHeld <= kRoom ? 2 : 1;
-    __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int row0, int pos, int step, bool *bad, int lane) {
+    __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int row0, int pos, int step, bool *bad, int lane,
+                        unsigned char *lds) {
         Tile t[kAhead];
         uint32_t valid[kAhead];
         int row[J];
-        if constexpr (!kSplit) init(a, it, g, row0, lane);
+        if constexpr (!kSplit) init(a, it, g, row0, lane, lds);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             look(a, it, b, g, pos + u * step, row, lane);
@@ -700,7 +729,7 @@ struct Rows16 {
             }
         }
         if constexpr (kSplit) {                               // splitting the queries takes a while: the keys come meanwhile
-            init(a, it, g, row0, lane);
+            init(a, it, g, row0, lane, lds);
             *bad |= odd_scale;
         }
         if (pos >= it.end) return;
