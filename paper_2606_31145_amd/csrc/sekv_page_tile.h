@@ -415,13 +415,44 @@ struct Rows16 {
     int lo[NB], hi[NB];                 // keys that the column's query sees
     int lo_all, hi_all, lo_any, hi_any; // keys that every column sees, that some column sees
 
+    // Queries that are split, on their way: a lane's own block of the only tile of rows; of two tiles whole rows, which LDS
+    // hands out.  Straight into the lanes a load would touch 64 lines at a time, eight times over.  With the stores of
+    // float_rows the same way: 16 float sequences of 900 keys, chunks of up to 100 tokens beside single ones, 60.0 us
+    // and KEEP1, 257 tokens over 9001 115.8 and KEEP2.  One tile has fewer rows mostly: one token of 32 sequences of up to 9000
+    // straight 65.2, through LDS 66.0.
+    static constexpr int kLanes = D / 4, kAsked = kSplit && NB == 2 ? 32 * kLanes / 64 : 8;     // lanes of a row, pieces a lane
+    typedef uint32_t w4v __attribute__((ext_vector_type(4)));
+    struct Asked { w4v w[kAsked]; };
+    __device__ static Asked ask(const PageAttendArgs &a, const Item &it, int g, int row0, int lane) {
+        Asked r;
+#pragma unroll
+        for (int i = 0; i < kAsked; ++i) {
+            int row = row0 + (NB == 2 ? i * (64 / kLanes) + lane / kLanes : lane & 15);
+            row = row < it.rows ? row : it.rows - 1;
+            const int gs = a.group_shift, piece = NB == 2 ? lane % kLanes : 8 * (lane >> 4) + i;
+            const float *src = static_cast<const float *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
+                               ((g << gs) + (row & ((1 << gs) - 1))) * D;
+            r.w[i] = w4v{0, 0, 0, 0};
+            if (piece < kLanes) r.w[i] = reinterpret_cast<const w4v *>(src)[piece];
+        }
+        return r;
+    }
+
     // Columns: rows row0 + 16 nb + lane % 16 of the item.
-    // lds: the wave's own, for 16 rows of floats (two tiles, split queries).
-    __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane, unsigned char *lds) {
+    // lds: the wave's own, for 32 rows of floats (where two tiles' queries were asked for).
+    __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane, const Asked &asked, unsigned char *lds) {
         const int n = lane & 15, gq = lane >> 4, gs = a.group_shift;
         const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
         using E = typename T::elem;
         odd_scale = false;
+        if constexpr (kSplit && NB == 2) {
+#pragma unroll
+            for (int i = 0; i < kAsked; ++i) {               // pieces sit at their index XOR the row's, for the banks
+                const int row = i * (64 / kLanes) + lane / kLanes;
+                *reinterpret_cast<w4v *>(lds + row * (D * 4) + ((lane % kLanes ^ (row & 7)) << 4)) = asked.w[i];
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             int row = row0 + 16 * nb + n;
@@ -433,37 +464,15 @@ struct Rows16 {
             const E *src = static_cast<const E *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
                            ((g << gs) + (row & ((1 << gs) - 1))) * D;
             if constexpr (kSplit) {
-                // Two tiles of rows: a load covers whole rows, and LDS hands each lane its block; straight into the lanes it
-                // would touch 64 lines at a time, eight times over.  With the stores of float_rows the same way: 16 float
-                // sequences of 900 keys, chunks of up to 100 tokens beside single ones, 60.0 us and 49.3, 257 tokens over
-                // 9001 115.8 and 113.4.  With one tile the rows are mostly fewer: one token of 32 sequences of up to 9000
-                // straight 65.2, through LDS 66.0.  Pieces of 16 bytes sit at their index XOR the row's, for the banks.
-                if constexpr (NB == 2) {
-                    constexpr int L = D / 4;                  // pieces, and lanes, of a row
-                    typedef uint32_t w4v __attribute__((ext_vector_type(4)));
-                    w4v w[16 * L / 64];
-#pragma unroll
-                    for (int i = 0; i < 16 * L / 64; ++i) {
-                        int at = row0 + 16 * nb + i * (64 / L) + lane / L;
-                        at = at < it.rows ? at : it.rows - 1;
-                        w[i] = reinterpret_cast<const w4v *>(static_cast<const E *>(a.q) + int64_t(it.tok0 + (at >> gs)) * a.q_stride +
-                                                             ((g << gs) + (at & ((1 << gs) - 1))) * D)[lane % L];
-                    }
-                    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                    for (int i = 0; i < 16 * L / 64; ++i) {
-                        const int at = i * (64 / L) + lane / L;
-                        *reinterpret_cast<w4v *>(lds + at * (D * 4) + ((lane % L ^ (at & 7)) << 4)) = w[i];
-                    }
-                    __builtin_amdgcn_wave_barrier();
-                }
                 typename Split32::f16v even, odd;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (D == 128 || gq < P::scales(D)) {
-                        if constexpr (NB == 2) w = *reinterpret_cast<const float4 *>(lds + n * (D * 4) + (((8 * gq + i) ^ (n & 7)) << 4));
-                        else w = reinterpret_cast<const float4 *>(src + 32 * gq)[i];
+                    float4 w;
+                    if constexpr (NB == 2) {
+                        w = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (8 * gq < kLanes) w = *reinterpret_cast<const float4 *>(lds + (16 * nb + n) * (D * 4) + (((8 * gq + i) ^ (n & 7)) << 4));
+                    } else {
+                        w = __builtin_bit_cast(float4, asked.w[i]);
                     }
                     even[2 * i] = w.x; odd[2 * i] = w.y; even[2 * i + 1] = w.z; odd[2 * i + 1] = w.w;
                 }
@@ -718,7 +727,9 @@ struct Rows16 {
         Tile t[kAhead];
         uint32_t valid[kAhead];
         int row[J];
-        if constexpr (!kSplit) init(a, it, g, row0, lane, lds);
+        Asked asked;
+        if constexpr (kSplit) asked = ask(a, it, g, row0, lane);
+        else init(a, it, g, row0, lane, asked, lds);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             look(a, it, b, g, pos + u * step, row, lane);
@@ -729,7 +740,7 @@ struct Rows16 {
             }
         }
         if constexpr (kSplit) {                               // splitting the queries takes a while: the keys come meanwhile
-            init(a, it, g, row0, lane, lds);
+            init(a, it, g, row0, lane, asked, lds);
             *bad |= odd_scale;
         }
         if (pos >= it.end) return;
