@@ -418,7 +418,7 @@ struct Rows16 {
     // Queries that are split, on their way: a lane's own block of the only tile of rows; of two tiles whole rows, which LDS
     // hands out.  Straight into the lanes a load would touch 64 lines at a time, eight times over.  With the stores of
     // float_rows the same way: 16 float sequences of 900 keys, chunks of up to 100 tokens beside single ones, 60.0 us
-    // and KEEP1, 257 tokens over 9001 115.8 and KEEP2.  One tile has fewer rows mostly: one token of 32 sequences of up to 9000
+    // and 49.1, 257 tokens over 9001 115.8 and 112.9.  One tile has fewer rows mostly: one token of 32 sequences of up to 9000
     // straight 65.2, through LDS 66.0.
     static constexpr int kLanes = D / 4, kAsked = kSplit && NB == 2 ? 32 * kLanes / 64 : 8;     // lanes of a row, pieces a lane
     typedef uint32_t w4v __attribute__((ext_vector_type(4)));
@@ -438,6 +438,18 @@ struct Rows16 {
         return r;
     }
 
+    // A lane's block from its eight pieces.
+    template <class F>
+    __device__ static bool split(F piece, Split32 *x) {
+        typename Split32::f16v even, odd;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 w = piece(i);
+            even[2 * i] = w.x; odd[2 * i] = w.y; even[2 * i + 1] = w.z; odd[2 * i + 1] = w.w;
+        }
+        return x->init(even, odd);
+    }
+
     // Columns: rows row0 + 16 nb + lane % 16 of the item.
     // lds: the wave's own, for 32 rows of floats (where two tiles' queries were asked for).
     __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane, const Asked &asked, unsigned char *lds) {
@@ -452,6 +464,19 @@ struct Rows16 {
                 *reinterpret_cast<w4v *>(lds + row * (D * 4) + ((lane % kLanes ^ (row & 7)) << 4)) = asked.w[i];
             }
             __builtin_amdgcn_wave_barrier();
+            // twice the same code, which is fetched anew in every launch: unrolled, with the stores of float_rows, 13 ragged float
+            // sequences 73.5 us instead of 72.7, 7 of which two are chunks 32.9 instead of 32.2
+#pragma unroll 1
+            for (int nb = 0; nb < 2; ++nb) {
+                Split32 x;
+                odd_scale |= split([&](int i) {
+                    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (8 * gq < kLanes) w = *reinterpret_cast<const float4 *>(lds + (16 * nb + n) * (D * 4) + (((8 * gq + i) ^ (n & 7)) << 4));
+                    return w;
+                }, &x);
+                if (nb == 0) qs[0] = x;
+                else qs[NB - 1] = x;
+            }
         }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -464,19 +489,7 @@ struct Rows16 {
             const E *src = static_cast<const E *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
                            ((g << gs) + (row & ((1 << gs) - 1))) * D;
             if constexpr (kSplit) {
-                typename Split32::f16v even, odd;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float4 w;
-                    if constexpr (NB == 2) {
-                        w = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (8 * gq < kLanes) w = *reinterpret_cast<const float4 *>(lds + (16 * nb + n) * (D * 4) + (((8 * gq + i) ^ (n & 7)) << 4));
-                    } else {
-                        w = __builtin_bit_cast(float4, asked.w[i]);
-                    }
-                    even[2 * i] = w.x; odd[2 * i] = w.y; even[2 * i + 1] = w.z; odd[2 * i + 1] = w.w;
-                }
-                odd_scale |= qs[nb].init(even, odd);
+                if constexpr (NB == 1) odd_scale |= split([&](int i) { return __builtin_bit_cast(float4, asked.w[i]); }, &qs[0]);
             }
 #pragma unroll
             for (int i = 0; i < (kSplit ? 0 : QW / 4); ++i) {
