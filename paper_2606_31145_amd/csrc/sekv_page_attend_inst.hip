@@ -138,7 +138,7 @@ __device__ inline bool float_rows(const PageAttendArgs &a, const Item &it, int b
 #pragma unroll
                 for (int e = 0; e < R::VE; ++e) so[(16 * nb + n) * RS + R::VE * (4 * gq + i) + e] = r.o[nb][e][i];
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_fence();
 #pragma unroll 2
         for (int r0 = 0; r0 < 32; r0 += 64 / GT) {
             const int row = r0 + lane / GT, rw = wave * 32 + row, d0 = lane % GT * 4;

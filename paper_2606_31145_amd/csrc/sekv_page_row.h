@@ -116,6 +116,13 @@ __device__ inline uint4 word_bf16(uint32_t w, float scale) {
     return make_uint4(pair_bf16<0>(w, scale), pair_bf16<1>(w, scale), pair_bf16<2>(w, scale), pair_bf16<3>(w, scale));
 }
 
+// LDS accesses of one wave complete in order; this keeps the compiler from moving one across the point where another
+// lane's value is needed.
+__device__ inline void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 __device__ inline void flag(const PageTables &t) {
     __hip_atomic_fetch_or(t.error, kErrPageRange, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }

@@ -463,7 +463,7 @@ struct Rows16 {
                 const int row = i * (64 / kLanes) + lane / kLanes;
                 *reinterpret_cast<w4v *>(lds + row * (D * 4) + ((lane % kLanes ^ (row & 7)) << 4)) = asked.w[i];
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_fence();
             // twice the same code, which is fetched anew in every launch: unrolled, with the stores of float_rows, 13 ragged float
             // sequences 73.5 us instead of 72.7, 7 of which two are chunks 32.9 instead of 32.2
 #pragma unroll 1

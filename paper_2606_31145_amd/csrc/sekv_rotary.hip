@@ -99,7 +99,7 @@ __device__ inline void turn_queries(const RotaryArgs &a, uint32_t item, double2 
     }
     if (a.positions) p = a.positions[tok];
     if (lane < a.rot_dim / 2) pairs[lane] = pair_of(a, double(p), freq);
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     Turn<T, D, kHalf> turn;
     turn.init(pairs, a.rot_dim, piece);
     for (int h = h0; h < h1; h += kSteps * kSide) {
@@ -149,13 +149,13 @@ __device__ inline void store_keys(const RotaryArgs &a, uint32_t item, double2 *p
     }
     double *where = reinterpret_cast<double *>(pairs + kRows * (D / 2));
     if (piece == 0) where[row] = p;
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     for (int i = lane; i - lane < kRows * R2; i += 64) {     // all lanes, for the frequencies are in them
         const int r = int(uint32_t(i) / uint32_t(R2));
         const double f = __shfl(freq, i - r * R2);
         if (i < kRows * R2) pairs[i] = pair_of(a, where[r], f);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     Turn<T, D, kHalf> turn;
     turn.init(pairs + row * R2, a.rot_dim, piece);
     for (int g = g0; g < g1; ++g) {
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
     __shared__ double2 pairs[kWaves][kPairs];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int64_t c = int64_t(blockIdx.x) * kWaves + wave; c < a.kv_items + a.q_items; c += int64_t(gridDim.x) * kWaves) {
-        __builtin_amdgcn_wave_barrier();
+        wave_fence();
         if constexpr (kPages) {
             if (c < a.kv_items) {
                 store_keys<T, P, D, kHalf>(a, uint32_t(c), pairs[wave], lane);
