@@ -486,8 +486,7 @@ SEKV_API sekv_status sekv_page_read(const sekv_page_dims *dims, const sekv_pages
  * Scores, and sums of values weighted by up to 2^8, are held in float (an item whose scores pass 2^26 in
  * magnitude is done row by row, some 300 times slower); with bfloat16 tokens the softmax weights are rounded to
  * bfloat16 for the matrix cores (off by at most 2^-8 of each); with float tokens nothing is.  Float tokens over
- * 4-bit pages: of each block of 32 values a query counts to 2^-24 of the block's largest, and an item with a block
- * whose largest is infinite, or below 2^-87 and not 0, is done row by row. */
+ * 4-bit pages: an item with a query value below 2^-102 and not 0 is done row by row, too. */
 SEKV_API sekv_status sekv_page_attend(const sekv_page_dims *dims, const sekv_pages *pages, const void *q,
                                       int64_t q_stride, const int32_t *tok_start, int32_t n_tokens,
                                       void *out, float *lse, void *ws, size_t ws_bytes, hipStream_t stream);

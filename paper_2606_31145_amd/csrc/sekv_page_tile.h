@@ -19,10 +19,18 @@
 namespace sekv {
 namespace page {
 
+typedef float f4v __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef __bf16 b8v __attribute__((ext_vector_type(8)));
 
 constexpr float kSlack = 8.f;
+
+typedef __attribute__((address_space(3))) unsigned char *lds_bytes;      // so that constant offsets stay in the instruction
+__device__ inline uint4 take16(lds_bytes p) {
+    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+    const u4v w = *(__attribute__((address_space(3))) const u4v *)p;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 
 // A weight is exp2(score * scale_log2 - m) in one fused step, while m is the rounded product of the largest score: that
 // one's weight is 2 to the product's rounding error instead of 1.  The error is common to all weights and does no
@@ -326,7 +334,7 @@ struct Keys16 {
     static constexpr bool kSplit = T::kBytes == 4 && P::kBytes == 0;          // sekv_page_split.h
     static constexpr int kBlocks = T::kBytes == 2 || kSplit ? 2 : 1, kKeys = 16 * kBlocks;
     static constexpr int kRow = P::row(D);
-    static constexpr int KW = kSplit ? 4 : kRow / 16, VW = kRow >= 64 ? kRow / 64 : 1;     // words a lane
+    static constexpr int KW = kRow / 16, VW = kRow >= 64 ? kRow / 64 : 1;     // words a lane
     uint32_t k[kBlocks][KW], v[kBlocks][4][VW], ks[kBlocks], vs[kBlocks];
 
     __device__ static size_t base(int row) { return row >= 0 ? row : 0; }     // any row: its keys are masked
@@ -336,16 +344,6 @@ struct Keys16 {
         for (int j = 0; j < kBlocks; ++j) {
             const size_t r0 = base(row[j]);
             const unsigned char *kp = static_cast<const unsigned char *>(a.k) + r0 * kRow;
-            if constexpr (kSplit) {                          // lane g: the row's block g, if it has one
-                uint4 w = make_uint4(0, 0, 0, 0);
-                ks[j] = 127;
-                if (D == 128 || g < P::scales(D)) {
-                    w = *reinterpret_cast<const uint4 *>(kp + m * kRow + 16 * g);
-                    ks[j] = a.k_scale[(r0 + m) * P::scales(D) + g];
-                }
-                k[j][0] = w.x; k[j][1] = w.y; k[j][2] = w.z; k[j][3] = w.w;
-                continue;
-            }
             if constexpr (KW == 2) {
                 const uint2 w = *reinterpret_cast<const uint2 *>(kp + m * kRow + 8 * g);
                 k[j][0] = w.x; k[j][1] = w.y;
@@ -404,23 +402,27 @@ struct Keys16 {
 template <class T, class P, int D, int NB>
 struct Rows16 {
     using Tile = Keys16<T, P, D>;
-    static constexpr int VE = D / 16, QW = T::kBytes == 2 ? D / 8 : D / 4;    // words of the query a lane
     static constexpr bool kBf = T::kBytes == 2, kSplit = Tile::kSplit;
+    // Pieces of a split query in registers; of two tiles the last pieces are in LDS, for the registers do not hold all.  The
+    // second ones there as well, with two groups of keys ahead instead: 2048 tokens over 8192 618 us instead of 594.
+    static constexpr int kHere = !kSplit ? 1 : NB == 1 ? 3 : 2;
+    static constexpr int VE = D / 16, QW = kBf ? D / 8 : kSplit ? kHere * (D / 8) : D / 4;     // words of the query a lane
     static constexpr int J = Tile::kBlocks;
-    uint32_t q[NB][kSplit ? 1 : QW];
-    Split32 qs[kSplit ? NB : 1];        // of the lane's block (zeros where a row has no block g)
-    bool odd_scale;                     // a block of queries that does not split
+    uint32_t q[NB][QW];
+    lds_bytes more;                     // kSplit: the lane's pieces in LDS
+    bool small;                         // kSplit: a query value that has no pieces
     f4v o[NB][VE];
     float m[NB], l[NB];
     int lo[NB], hi[NB];                 // keys that the column's query sees
     int lo_all, hi_all, lo_any, hi_any; // keys that every column sees, that some column sees
 
-    // Queries that are split, on their way: a lane's own block of the only tile of rows; of two tiles whole rows, which LDS
-    // hands out.  Straight into the lanes a load would touch 64 lines at a time, eight times over.  With the stores of
-    // float_rows the same way: 16 float sequences of 900 keys, chunks of up to 100 tokens beside single ones, 60.0 us
+    // Queries that are cut into pieces, on their way: a lane's own D / 4 values of the only tile of rows; of two tiles whole
+    // rows, which LDS hands out.  Straight into the lanes a load would touch 64 lines at a time, eight times over.  With the
+    // stores of float_rows the same way: 16 float sequences of 900 keys, chunks of up to 100 tokens beside single ones, 60.0 us
     // and 49.1, 257 tokens over 9001 115.8 and 112.9.  One tile has fewer rows mostly: one token of 32 sequences of up to 9000
     // straight 65.2, through LDS 66.0.
-    static constexpr int kLanes = D / 4, kAsked = kSplit && NB == 2 ? 32 * kLanes / 64 : 8;     // lanes of a row, pieces a lane
+    static constexpr int kLanes = D / 4, kOwn = kLanes / 4;     // 16-byte pieces of a row, of a lane's values
+    static constexpr int kAsked = kSplit && NB == 2 ? 32 * kLanes / 64 : kOwn;
     typedef uint32_t w4v __attribute__((ext_vector_type(4)));
     struct Asked { w4v w[kAsked]; };
     __device__ static Asked ask(const PageAttendArgs &a, const Item &it, int g, int row0, int lane) {
@@ -429,55 +431,72 @@ struct Rows16 {
         for (int i = 0; i < kAsked; ++i) {
             int row = row0 + (NB == 2 ? i * (64 / kLanes) + lane / kLanes : lane & 15);
             row = row < it.rows ? row : it.rows - 1;
-            const int gs = a.group_shift, piece = NB == 2 ? lane % kLanes : 8 * (lane >> 4) + i;
+            const int gs = a.group_shift, piece = NB == 2 ? lane % kLanes : kOwn * (lane >> 4) + i;
             const float *src = static_cast<const float *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
                                ((g << gs) + (row & ((1 << gs) - 1))) * D;
-            r.w[i] = w4v{0, 0, 0, 0};
-            if (piece < kLanes) r.w[i] = reinterpret_cast<const w4v *>(src)[piece];
+            r.w[i] = reinterpret_cast<const w4v *>(src)[piece];
         }
         return r;
     }
 
-    // A lane's block from its eight pieces.
-    template <class F>
-    __device__ static bool split(F piece, Split32 *x) {
-        typename Split32::f16v even, odd;
+    // A tile's pieces from the lane's values, in the order in which Keys16 lays out keys: into registers, and the others into
+    // the lane's places of LDS, 16 bytes of each kilobyte.
+    static constexpr int kProducts = D / 32, kMore = kProducts * (kPieces - kHere) * 1024;    // of a tile of rows
+    __device__ static bool cut(const w4v (&v)[kOwn], uint32_t (&here)[QW], unsigned char *to) {
+        bool small = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 w = piece(i);
-            even[2 * i] = w.x; odd[2 * i] = w.y; even[2 * i + 1] = w.z; odd[2 * i + 1] = w.w;
+        for (int i = 0; i < kProducts; ++i) {
+            uint32_t w[4][kPieces];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const w4v x = v[2 * i + u / 2];
+                const float a = __uint_as_float(x[u % 2 * 2]), b = __uint_as_float(x[u % 2 * 2 + 1]);
+                cut2(a, b, w[u]);
+                small |= too_small(a) | too_small(b);
+#pragma unroll
+                for (int p = 0; p < kHere; ++p) here[p * (D / 8) + 4 * i + u] = w[u][p];
+            }
+#pragma unroll
+            for (int p = kHere; p < kPieces; ++p)
+                *reinterpret_cast<w4v *>(to + ((p - kHere) * kProducts + i) * 1024) = w4v{w[0][p], w[1][p], w[2][p], w[3][p]};
         }
-        return x->init(even, odd);
+        return small;
     }
 
     // Columns: rows row0 + 16 nb + lane % 16 of the item.
-    // lds: the wave's own, for 32 rows of floats (where two tiles' queries were asked for).
+    // lds: the wave's own, for 16 NB rows of floats (kSplit), which the pieces fill as well.
     __device__ void init(const PageAttendArgs &a, const Item &it, int g, int row0, int lane, const Asked &asked, unsigned char *lds) {
         const int n = lane & 15, gq = lane >> 4, gs = a.group_shift;
         const int64_t cap = int64_t(a.t.max_pages) << a.t.page_shift;
         using E = typename T::elem;
-        odd_scale = false;
+        small = false;
+        more = (lds_bytes)lds + lane * 16;
         if constexpr (kSplit && NB == 2) {
 #pragma unroll
             for (int i = 0; i < kAsked; ++i) {               // pieces sit at their index XOR the row's, for the banks
                 const int row = i * (64 / kLanes) + lane / kLanes;
                 *reinterpret_cast<w4v *>(lds + row * (D * 4) + ((lane % kLanes ^ (row & 7)) << 4)) = asked.w[i];
             }
-            wave_fence();
             // twice the same code, which is fetched anew in every launch: unrolled, with the stores of float_rows, 13 ragged float
             // sequences 73.5 us instead of 72.7, 7 of which two are chunks 32.9 instead of 32.2
 #pragma unroll 1
             for (int nb = 0; nb < 2; ++nb) {
-                Split32 x;
-                odd_scale |= split([&](int i) {
-                    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (8 * gq < kLanes) w = *reinterpret_cast<const float4 *>(lds + (16 * nb + n) * (D * 4) + (((8 * gq + i) ^ (n & 7)) << 4));
-                    return w;
-                }, &x);
-                if (nb == 0) qs[0] = x;
-                else qs[NB - 1] = x;
+                w4v v[kOwn];
+                uint32_t x[QW];
+                wave_fence();
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i)
+                    v[i] = *reinterpret_cast<const w4v *>(lds + (16 * nb + n) * (D * 4) + (((kOwn * gq + i) ^ (n & 7)) << 4));
+                wave_fence();                                // a tile's pieces lie where its rows did
+                small |= cut(v, x, lds + lane * 16 + nb * kMore);
+#pragma unroll
+                for (int i = 0; i < QW; ++i) {
+                    if (nb == 0) q[0][i] = x[i];
+                    else q[NB - 1][i] = x[i];
+                }
             }
         }
+        if constexpr (kSplit && NB == 1) small = cut(asked.w, q[0], lds + lane * 16);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             int row = row0 + 16 * nb + n;
@@ -488,9 +507,6 @@ struct Rows16 {
             hi[nb] = int(p < 0 ? -1 : p < cap ? p : cap - 1);
             const E *src = static_cast<const E *>(a.q) + int64_t(it.tok0 + (row >> gs)) * a.q_stride +
                            ((g << gs) + (row & ((1 << gs) - 1))) * D;
-            if constexpr (kSplit) {
-                if constexpr (NB == 1) odd_scale |= split([&](int i) { return __builtin_bit_cast(float4, asked.w[i]); }, &qs[0]);
-            }
 #pragma unroll
             for (int i = 0; i < (kSplit ? 0 : QW / 4); ++i) {
                 // the dims of product i: as Keys16 lays out its pieces
@@ -526,19 +542,45 @@ struct Rows16 {
             return codes8_bf16(t.k[j][2 * s], t.k[j][2 * s + 1], pow2_of(t.ks[j]));
         }
     }
+    // The sum over all pieces, smaller ones first.
+    __device__ void split_scores(const Tile &t, f4v (&s)[J][NB]) const {
+        lds_bytes at = more;
+        asm volatile("" : "+v"(at));                         // read in every step: kept in registers they do not fit
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) s[j][nb] = f4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kProducts; ++i) {
+            uint4 kf[J];
+#pragma unroll
+            for (int j = 0; j < J; ++j) kf[j] = word_bf16(t.k[j][i], pow2_of(t.ks[j]));
+#pragma unroll
+            for (int p = kPieces - 1; p >= 0; --p)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const int r = p < kHere ? p * (D / 8) + 4 * i : 0;
+                    uint4 w = make_uint4(q[nb][r], q[nb][r + 1], q[nb][r + 2], q[nb][r + 3]);
+                    if (p >= kHere) w = take16(at + nb * kMore + ((p - kHere) * kProducts + i) * 1024);
+#pragma unroll
+                    for (int j = 0; j < J; ++j) s[j][nb] = mma16(kf[j], w, s[j][nb]);
+                }
+        }
+    }
     // Float scores in several sums, so that fewer roundings follow each other: one chain of D terms put a single
     // token's output 7.6e-7 off (root mean square over 100 inputs of 2048 keys), two chains 4.5e-7, four 3.4e-7,
     // at the same time; with two tiles of rows four cost 1 % more than two.
     static constexpr int kSums = NB == 1 ? 4 : 2;
     __device__ void scores(const Tile &t, f4v (&s)[Tile::kBlocks][NB]) const {
+        if constexpr (kSplit) {
+            split_scores(t, s);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < Tile::kBlocks; ++j) {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) s[j][nb] = f4v{0.f, 0.f, 0.f, 0.f};
-            if constexpr (kSplit) {
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) s[j][nb] = mma_split(t.k[j], t.ks[j], qs[nb], s[j][nb]);
-            } else if constexpr (kBf) {
+            if constexpr (kBf) {
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
                     const uint4 kf = k_frag(t, j, i);
@@ -732,7 +774,7 @@ struct Rows16 {
     // ahead; its row blocks one group before that.  Two groups where they fit: 32 ragged sequences in bfloat16 462 us
     // against 469 with one, 4 of 131072 in 8 bits 188.6 against 191.2, 13 of float and head_dim 64 577 against 599.
     // In 4 bits three: 32 ragged sequences 168.7 us against 173.4 with two, 167.8 with four, 4 of 131072 109.9, 109.5, 110.6.
-    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 2 : 0)), kHeld = NB * (D / 4 + (kSplit ? 6 * kPieces + 2 : QW));
+    static constexpr int kTileWords = J * (Tile::KW + 4 * Tile::VW + (P::kBytes == 0 ? 2 : 0)), kHeld = NB * (D / 4 + QW);
     static constexpr int kRoom = kSplit ? 150 : 176;                          // of 256 registers
     static constexpr int kAhead = P::kBytes == 0 && 3 * kTileWords + kHeld <= kRoom ? 3 : 2 * kTileWords + kHeld <= kRoom ? 2 : 1;
     __device__ void run(const PageAttendArgs &a, const Item &it, int b, int g, int row0, int pos, int step, bool *bad, int lane,
@@ -752,9 +794,9 @@ struct Rows16 {
                 t[u].load_values(a, row, lane);
             }
         }
-        if constexpr (kSplit) {                               // splitting the queries takes a while: the keys come meanwhile
+        if constexpr (kSplit) {                               // cutting the queries takes a while: the keys come meanwhile
             init(a, it, g, row0, lane, asked, lds);
-            *bad |= odd_scale;
+            *bad |= small;
         }
         if (pos >= it.end) return;
         for (;;) {

@@ -31,16 +31,10 @@ namespace page {
 
 // Four rows of one column of a bf16 tile in LDS: within 16 lanes, lane i names 4 columns
 // 4 (i % 4) of row i / 4 and receives column i of the four rows.
-typedef __attribute__((address_space(3))) unsigned char *lds_bytes;      // so that constant offsets stay in the instruction
 __device__ inline uint2 turn4(lds_bytes p) {
     typedef short s4v __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s4v *lds_p;
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)p));
-}
-__device__ inline uint4 take16(lds_bytes p) {
-    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
-    const u4v w = *(__attribute__((address_space(3))) const u4v *)p;
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <int D> struct Swizzle {
     static constexpr int CH = D / 8;                   // 16-byte pieces a row
