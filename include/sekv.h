@@ -420,7 +420,7 @@ SEKV_API sekv_status sekv_page_append(const sekv_page_dims *dims, const sekv_pag
  *   x' = scale (x cos a - y sin a),  y' = scale (y cos a + x sin a),
  * over the first rot_dim values of a head; those behind stay as they are.  Pairs are (i, i + rot_dim / 2) in
  * the half layout, (2 i, 2 i + 1) in the interleaved one.  Angles, their cosines and the products are formed
- * in double and rounded to float, and that to the rows' type. */
+ * in double and rounded to float, and that to the rows' type.  Angles from 2^50 quarter turns (1.76e15) on give NaN. */
 typedef enum { SEKV_ROTARY_HALF = 0, SEKV_ROTARY_INTERLEAVED = 1 } sekv_rotary_layout;
 typedef struct {
     int32_t rot_dim;        /* a multiple of 16, at most head_dim                          */

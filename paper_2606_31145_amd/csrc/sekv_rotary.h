@@ -12,11 +12,15 @@ namespace sekv {
 namespace page {
 
 // (cos, sin) of an angle.  k quarter turns are taken off with pi / 2 in two parts, each product exact within its fused
-// step, so that what is left is as exact as the angle for every k that a double counts; then the series up to x^15 and
-// x^16, whose next terms are below 2^-54 at pi / 4.
+// step, so that what is left is as exact as the angle; then the series up to x^15 and x^16, whose next terms are below
+// 2^-54 at pi / 4.  Up to 2^50 quarter turns the quotient's rounding leaves k at most an eighth beside the nearest one, and
+// the next terms below 2^-47; angles past that, which a double holds to a quarter at best, are no number.
 __device__ inline double2 cos_sin(double angle) {
-    const double k = __builtin_rint(angle * 0.63661977236758134308);
-    const double r = fma(-k, 6.123233995736766036e-17, fma(-k, 1.57079632679489661923, angle)), z = r * r;
+    double k = __builtin_rint(angle * 0.63661977236758134308);
+    const bool far = !(fabs(k) < 1125899906842624.0);
+    k = far ? 0.0 : k;
+    const double left = fma(-k, 6.123233995736766036e-17, fma(-k, 1.57079632679489661923, angle));
+    const double r = far ? __builtin_nan("") : left, z = r * r;
     double s = -1.0 / 1307674368000.0;
     s = fma(s, z, 1.0 / 6227020800.0);
     s = fma(s, z, -1.0 / 39916800.0);
