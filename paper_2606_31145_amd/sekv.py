@@ -933,7 +933,37 @@ class Rotary:
 
 def rotate(x, positions, rotary: Rotary, out=None, transpose: bool = False, stream=None):
     """sekv_rotate: x [n_tokens][heads][d] (tokens may be strided; float32 or bfloat16) turned by positions int32
-    [n_tokens]; out may be x itself.  transpose: the other way, which is the gradient with respect to x."""
+    [n_tokens]; out may be x itself.  transpose: the other way, which is the gradient with respect to x.  Where x requires
+    a gradient the result has one, of any order; out cannot be given then."""
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (x, out)):
+        if out is not None:
+            raise ValueError("out: no gradient passes through a tensor that is given")
+        with _on(x.device, stream, "rows")[0]:               # so that the backward pass runs on this stream, too
+            return _Rotate.apply(x, positions, rotary, bool(transpose))
+    return _rotate(x, positions, rotary, out, transpose, stream)
+
+
+class _Rotate(torch.autograd.Function):
+    """The turn the other way is the gradient."""
+
+    @staticmethod
+    def forward(ctx, x, positions, rotary, transpose):
+        y = _rotate(x, positions, rotary, None, transpose, None)
+        ctx.save_for_backward(positions, rotary.freq)        # whoever changes them meanwhile is told
+        ctx.call = rotary, not transpose
+        return y
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, _ = ctx.saved_tensors
+        rotary, transpose = ctx.call
+        grad = grad.contiguous()
+        if grad.data_ptr() % 16:
+            grad = grad.clone()
+        return rotate(grad, positions, rotary, transpose=transpose), None, None, None
+
+
+def _rotate(x, positions, rotary, out, transpose, stream):
     if not isinstance(x, torch.Tensor) or x.dim() != 3 or x.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("x: float32 or bfloat16 [n_tokens][heads][d]")
     _, heads, d = x.shape
