@@ -389,6 +389,7 @@ sekv_status rotary_frequencies(const sekv_rotary_spec *p, double *freq, double *
     if (p->scaling == SEKV_ROTARY_BASE && p->rot_dim == 2)
         return fail(SEKV_ERR_UNSUPPORTED, "a stretched base needs two pairs at least");
     const double base = p->scaling == SEKV_ROTARY_BASE ? p->base * std::pow(p->factor, R / (R - 2.0)) : p->base;
+    if (!std::isfinite(base)) return fail(SEKV_ERR_UNSUPPORTED, "base %g stretched by %g has no number", p->base, p->factor);
     // the pair, as a real number, that turns so many times over the trained positions
     auto pair_of = [&](double turns) { return R * std::log(p->trained / (turns * two_pi)) / (2.0 * std::log(p->base)); };
     double from = 0.0, to = 0.0;
