@@ -89,16 +89,7 @@ sekv::PageTables tables(const sekv_page_dims *d, const sekv_pages *p, const int3
     return t;
 }
 
-// Work items aimed at: two workgroups a compute unit, two rounds of them, so that ragged chunks even out.
-// A workgroup without an item still has to be started and to find that out.  Measured (us) with 512, 1024
-// and 2048: one token of 8 sequences at 9000 in 8 bits 30.6, 30.5, 34.0; six of 16 under a window 30.8,
-// 30.9, 32.8; one of 32 ragged sequences of up to 32768 in bfloat16 511, 465, 453; one of 5 of up to 131072
-// in 8 bits 218, 188, 191; 9 ragged ones, one of 300 tokens, 467, 425, 434.
-constexpr int kItems = 1024;
-// In 4 bits an item is shorter and ragged ends weigh more.  With 1024, 1280 and 1536: one token of 32 ragged sequences of
-// up to 32768 169, 159, 162, of 64 of up to 4096 53.8, 53.9, 57.7, of 8 at 9000 22.9, 24.3, 25.2.
-constexpr int kItems4 = 1280;
-int items_of(const sekv_page_dims *d) { return d->page_dtype == SEKV_E2M1 ? kItems4 : kItems; }
+int items_of(const sekv_page_dims *d) { return sekv::page::items_of(d->page_dtype == SEKV_E2M1); }
 
 sekv::page::Launch plan(const sekv_page_dims *d, int n_tokens) {
     return sekv::page::plan_launch(d->batch, n_tokens, d->n_kv_heads, log2_of(d->n_q_heads / d->n_kv_heads),

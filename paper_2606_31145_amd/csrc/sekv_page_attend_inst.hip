@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
                 (s.nq && a.t.seq_len[b] > cap))
                 flag(a.t);
         }
-    const Plan plan = make_plan(a, T::kBytes == 4, P::kBytes == 0, lane, lds);
+    const Plan plan = make_plan<T, P>(a, lane, lds);
     int b = 0, c = 0, g = 0;
     const uint32_t x = place_of(blockIdx.x, a.t.Hkv, &g);
     Item it;
@@ -315,12 +315,12 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
 
 // Joins the partials of as many rows of a tile at a time as a workgroup holds side by side.
 constexpr int join_parts(int D) { return kTileRows / (kThreads / (D / 4)); }
-template <class T, int D>
+template <class T, class P, int D>
 __global__ void __launch_bounds__(kThreads) join_kernel(PageAttendArgs a) {
     constexpr int kParts = join_parts(D), kRows = kTileRows / kParts;
     __shared__ __attribute__((aligned(16))) unsigned char lds[256 * (sizeof(float4) + sizeof(float2))];
     const int lane = threadIdx.x & 63;
-    const Plan plan = make_plan(a, T::kBytes == 4, false, lane, lds);
+    const Plan plan = make_plan<T, P>(a, lane, lds);
     if (!plan.chunk || plan.longest <= plan.chunk) return;   // nothing was cut
     const int64_t all = int64_t(plan.tiles) * a.t.Hkv * kParts;
     for (int64_t u = blockIdx.x; u < all; u += gridDim.x) {
@@ -346,7 +346,7 @@ hipError_t SEKV_NAME(SEKV_T, SEKV_P, SEKV_D)(const PageAttendArgs &a, hipStream_
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1 || !a.join_launch) return e;
     const int64_t parts = a.tiles * a.t.Hkv * join_parts(SEKV_D);
-    hipLaunchKernelGGL((join_kernel<T, SEKV_D>), dim3(unsigned(parts < kJoinBlocks ? parts : kJoinBlocks)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((join_kernel<T, P, SEKV_D>), dim3(unsigned(parts < kJoinBlocks ? parts : kJoinBlocks)), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -124,6 +124,20 @@ SEKV_HD int chunk_length(uint64_t W, int T, int max_len, int Hkv, int target, in
     const uint32_t r = uint32_t(c > (1u << 30) ? (1u << 30) : c);
     return int((r + kChunkStep - 1) / kChunkStep * kChunkStep);
 }
+// The chunk length of a call, by its storage (`four`: 4-bit pages) and the way its partials are joined: every kernel of the
+// call asks here, for one reads at the chunk borders where another wrote.
+SEKV_HD int call_chunk(uint64_t W, int T, int max_len, int Hkv, int target, int splits, int n_tokens, int group_shift,
+                       bool join_launch, bool is_float, bool four) {
+    const float rows = join_rows_of(join_launch, n_tokens, group_shift, T);
+    return chunk_length(W, T, max_len, Hkv, target, splits, four && !join_launch ? kOver4 : over_of(join_launch, is_float),
+                        four ? kJoin4 * rows : rows);
+}
+// Where sequence `lane` of up to 64 stands when those of wide tiles, a bit each, come first and both kinds keep their order.
+SEKV_HD int wide_first(uint64_t wide, int lane) {
+    const uint64_t before = (uint64_t(1) << lane) - 1;
+    return wide >> lane & 1 ? __builtin_popcountll(wide & before)
+                            : __builtin_popcountll(wide) + __builtin_popcountll(~wide & before);
+}
 SEKV_HD int chunks_of(const Seq &s, int chunk) { return s.len > chunk ? (s.len + chunk - 1) / chunk : 1; }
 
 // What one item covers.
@@ -170,6 +184,17 @@ SEKV_HD Item make_item(const Seq &s, int tile, int c, int chunk, int64_t cap, in
 // Whether some row of the item sees a key of the block at pos.  An item begins at a multiple of 64, so under a
 // window its first blocks may lie before every row's: their page may be somebody else's by then, or none.
 SEKV_HD bool block_seen(const Item &it, int pos) { return pos < it.end && pos + kBlock > it.first; }
+
+// Work items aimed at: two workgroups a compute unit, two rounds of them, so that ragged chunks even out.
+// A workgroup without an item still has to be started and to find that out.  Measured (us) with 512, 1024
+// and 2048: one token of 8 sequences at 9000 in 8 bits 30.6, 30.5, 34.0; six of 16 under a window 30.8,
+// 30.9, 32.8; one of 32 ragged sequences of up to 32768 in bfloat16 511, 465, 453; one of 5 of up to 131072
+// in 8 bits 218, 188, 191; 9 ragged ones, one of 300 tokens, 467, 425, 434.
+constexpr int kItems = 1024;
+// In 4 bits an item is shorter and ragged ends weigh more.  With 1024, 1280 and 1536: one token of 32 ragged sequences of
+// up to 32768 169, 159, 162, of 64 of up to 4096 53.8, 53.9, 57.7, of 8 at 9000 22.9, 24.3, 25.2.
+constexpr int kItems4 = 1280;
+SEKV_HD int items_of(bool four) { return four ? kItems4 : kItems; }
 
 // Host side: grid and workspace of a call.
 struct Launch {

@@ -103,7 +103,8 @@ struct Plan {
 };
 
 // lds: 256 bytes, free again on return.
-__device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, bool four, int lane, unsigned char *lds) {
+template <class Tokens, class Pages>
+__device__ inline Plan make_plan(const PageAttendArgs &a, int lane, unsigned char *lds) {
     Plan p;
     uint64_t W = 0;
     int mx = 0, T = 0;
@@ -158,9 +159,8 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, bool is_float, bool fo
     W = __builtin_amdgcn_readfirstlane(uint32_t(W)) | uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(W >> 32))) << 32;
     p.tiles = __builtin_amdgcn_readfirstlane(T);
     p.longest = __builtin_amdgcn_readfirstlane(mx);
-    const float rows = join_rows_of(a.join_launch, a.t.n_tokens, a.group_shift, p.tiles);
-    p.chunk = chunk_length(W, p.tiles, p.longest, a.t.Hkv, a.target, a.splits,
-                           four && !a.join_launch ? kOver4 : over_of(a.join_launch, is_float), four ? kJoin4 * rows : rows);
+    p.chunk = call_chunk(W, p.tiles, p.longest, a.t.Hkv, a.target, a.splits, a.t.n_tokens, a.group_shift, a.join_launch != 0,
+                         Tokens::kBytes == 4, Pages::kBytes == 0);
     return p;
 }
 
@@ -189,8 +189,7 @@ __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, 
     if constexpr (kWideFirst) {
         const unsigned long long wide = __ballot(!many && lane < a.t.B && (p.mine.nq << a.group_shift) > kFewRows);
         if (wide) {
-            const unsigned long long before = (1ull << lane) - 1;
-            const int to = wide >> lane & 1 ? __popcll(wide & before) : __popcll(wide) + __popcll(~wide & before);
+            const int to = wide_first(wide, lane);
             n = __builtin_amdgcn_ds_permute(to << 2, n);
             whose = __builtin_amdgcn_ds_permute(to << 2, lane);
         }
