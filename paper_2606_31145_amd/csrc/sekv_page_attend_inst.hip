@@ -8,7 +8,7 @@
 //
 // What bounds it: few rows, the keys' and values' bytes (sekv_page_tile.h); 128 bfloat16 rows, the matrix cores
 // and the softmax's vector instructions in turn (sekv_page_wide.h); float rows, the float matrix instruction, over 4-bit
-// pages the vector instructions that split weights and scale values (sekv_page_split.h).
+// pages the vector instructions that split weights and scale keys and values (sekv_page_split.h).
 // The smallest calls are a chain of dependent reads (tables, page, rows, partials): one token over 2048 keys,
 // which are 0.2 us of bytes, spends 3.0 us until its workgroups know the plan, 0.6 on finding their items, 3.4 on
 // keys and values and 3.2 on the join.
@@ -30,8 +30,8 @@ using namespace page;
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int64_t kJoinBlocks = 2048;      // eight on each compute unit
 
-// __syncthreads_or for a workgroup's one question.  The library's keeps all of a thread's indices in a register until then,
-// which the float form of 4-bit keys does not have to spare.
+// __syncthreads_or for a workgroup's one question, over 4-bit pages, whose items are the shortest: one token over 2048 keys
+// takes 8.95 us with this and 9.1 with the library's.
 __device__ inline bool any_thread(bool x, int lane, int wave) {
     __shared__ uint32_t told[kWaves];
     const bool here = __any(x);
@@ -109,18 +109,13 @@ __device__ inline bool narrow(const PageAttendArgs &a, const Item &it, int b, in
     return join_waves<T, P, D, NB>(a, it, r, bad, g, c, lane, wave, lds);
 }
 
-// Up to 128 float rows: 32 to a wave, which reads all the item's keys.  Over 4-bit pages up to 32 as well, as in narrow:
-// in one piece of code, for with two of them the kernels of a call are past the instruction cache's 64 KB: 2048 tokens over
-// 8192 keys 506 us against 520, 257 over 9001 115.8 against 118.
+// Up to 128 float rows: 32 to a wave, which reads all the item's keys.
 template <class P, int D>
 __device__ inline bool float_rows(const PageAttendArgs &a, const Item &it, int b, int g, int c, int lane, int wave, unsigned char *lds) {
     using R = Rows16<F32, P, D, 2>;
     R r;
     bool bad = false;
-    const bool few = P::kBytes == 0 && it.narrow;
-    const int row0 = few ? 0 : wave * 32, at = few ? wave : 0, of = few ? kWaves : 1;
-    if (row0 < it.rows) r.run(a, it, b, g, row0, it.begin + at * R::Tile::kKeys, of * R::Tile::kKeys, &bad, lane, own_rows<D, 2>(lds, wave));
-    if (few) return join_waves<F32, P, D, 2>(a, it, r, bad, g, c, lane, wave, lds);
+    if (wave * 32 < it.rows) r.run(a, it, b, g, wave * 32, it.begin, R::Tile::kKeys, &bad, lane, own_rows<D, 2>(lds, wave));
     if (any_of<P>(bad, lane, wave)) return true;
     if (wave * 32 >= it.rows) return false;
     const int n = lane & 15, gq = lane >> 4;
@@ -294,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_kernel(PageAttendArgs a) {
     if (!plan.chunk || !find_item<false, P::kBytes == 0>(a, x, lane, plan, lds, &b, &c, &it)) return;
     bool again;
     if (it.narrow && it.rows <= 16) again = narrow<T, P, D, 1>(a, it, b, g, c, lane, wave, lds);
-    else if (it.narrow && (T::kBytes == 2 || P::kBytes != 0)) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);
+    else if (it.narrow) again = narrow<T, P, D, 2>(a, it, b, g, c, lane, wave, lds);
     else if constexpr (T::kBytes == 2) again = wide_bf16<P, D>(a, it, b, g, c, lane, wave, lds);
     else again = float_rows<P, D>(a, it, b, g, c, lane, wave, lds);
     if (again) plain_rows<T, P, D>(a, it, b, g, c, lane, wave);

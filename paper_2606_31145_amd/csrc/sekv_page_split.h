@@ -6,7 +6,7 @@
 // exact, so what is left are the roundings of float sums.
 //
 // Three pieces a product still take a fifth of the float instruction's time.  2048 tokens over 8192 keys, head_dim 128: 2033 us
-// with the float instruction on converted codes, 594 so (405 TFLOP/s); 257 over 9001 380 and 127.  Pieces of 6 bits that share
+// with the float instruction on converted codes, 587 so (410 TFLOP/s); 257 over 9001 380 and 126.  Pieces of 6 bits that share
 // a block's exponent, on the instruction for low precisions, took 506 and 112, but a value beside one 2^10 times larger
 // kept 14 of its bits.
 #pragma once

@@ -168,8 +168,8 @@ __device__ inline Plan make_plan(const PageAttendArgs &a, int lane, unsigned cha
 // tokens of a chunk see more keys).  kTiles: tile x instead, as its first chunk's item.  x and so the result are
 // the same in all threads.  lds as above.
 // kWideFirst: of up to 64 sequences those of wide tiles come first, whose items last longest: they start on compute units
-// of their own, and the short ones join them.  Over 4-bit pages (us): 7 ragged sequences, two of them chunks, in float 38.8
-// in order and 32.8 so, 13 of which one has 257 tokens 141 and 131, 32 of up to 2000 100 and 85; with no wide tile 8.9 and 9.0.
+// of their own, and the short ones join them.  Over 4-bit pages (us): 7 ragged sequences, two of them chunks, in float 39.7
+// in order and 32.9 so, 13 of which one has 257 tokens 141 and 131, 32 of up to 2000 100 and 85; with no wide tile 8.9 and 9.0.
 // In 8 bits 13 sequences 90.4 and 90.6: there the order stays.
 template <bool kTiles = false, bool kWideFirst = false>
 __device__ inline bool find_item(const PageAttendArgs &a, uint32_t x, int lane, const Plan &p, unsigned char *lds, int *b_out,
@@ -403,7 +403,7 @@ struct Rows16 {
     using Tile = Keys16<T, P, D>;
     static constexpr bool kBf = T::kBytes == 2, kSplit = Tile::kSplit;
     // Pieces of a split query in registers; of two tiles the last pieces are in LDS, for the registers do not hold all.  The
-    // second ones there as well, with two groups of keys ahead instead: 2048 tokens over 8192 618 us instead of 594.
+    // second ones there as well, with two groups of keys ahead instead: 2048 tokens over 8192 616 us instead of 592.
     static constexpr int kHere = !kSplit ? 1 : NB == 1 ? 3 : 2;
     static constexpr int VE = D / 16, QW = kBf ? D / 8 : kSplit ? kHere * (D / 8) : D / 4;     // words of the query a lane
     static constexpr int J = Tile::kBlocks;
@@ -417,9 +417,8 @@ struct Rows16 {
 
     // Queries that are cut into pieces, on their way: a lane's own D / 4 values of the only tile of rows; of two tiles whole
     // rows, which LDS hands out.  Straight into the lanes a load would touch 64 lines at a time, eight times over.  With the
-    // stores of float_rows the same way: 16 float sequences of 900 keys, chunks of up to 100 tokens beside single ones, 60.0 us
-    // and 49.1, 257 tokens over 9001 115.8 and 112.9.  One tile has fewer rows mostly: one token of 32 sequences of up to 9000
-    // straight 65.2, through LDS 66.0.
+    // stores of float_rows the same way: 16 float sequences of 900 keys, chunks of up to 100 tokens beside single ones, 61.2 us
+    // and 49.6, 257 tokens over 9001 130.9 and 126.8.  One tile has fewer rows mostly and gains nothing by it.
     static constexpr int kLanes = D / 4, kOwn = kLanes / 4;     // 16-byte pieces of a row, of a lane's values
     static constexpr int kAsked = kSplit && NB == 2 ? 32 * kLanes / 64 : kOwn;
     typedef uint32_t w4v __attribute__((ext_vector_type(4)));
@@ -477,7 +476,7 @@ struct Rows16 {
                 *reinterpret_cast<w4v *>(lds + row * (D * 4) + ((lane % kLanes ^ (row & 7)) << 4)) = asked.w[i];
             }
             // twice the same code, which is fetched anew in every launch: unrolled, with the stores of float_rows, 13 ragged float
-            // sequences 73.5 us instead of 72.7, 7 of which two are chunks 32.9 instead of 32.2
+            // sequences 77.8 us instead of 77.2, 7 of which two are chunks 33.6 instead of 32.9
 #pragma unroll 1
             for (int nb = 0; nb < 2; ++nb) {
                 w4v v[kOwn];

@@ -13,8 +13,8 @@ namespace page {
 
 // (cos, sin) of an angle.  k quarter turns are taken off with pi / 2 in two parts, each product exact within its fused
 // step, so that what is left is as exact as the angle; then the series up to x^15 and x^16, whose next terms are below
-// 2^-54 at pi / 4.  Up to 2^50 quarter turns the quotient's rounding leaves k at most an eighth beside the nearest one, and
-// the next terms below 2^-47; angles past that, which a double holds to a quarter at best, are no number.
+// 2^-54 at pi / 4.  Up to 2^50 quarter turns the quotient's roundings leave k at most a fifth beside the nearest one, and
+// the next terms below 2^-46; angles past that, which a double holds to a quarter at best, are no number.
 __device__ inline double2 cos_sin(double angle) {
     double k = __builtin_rint(angle * 0.63661977236758134308);
     const bool far = !(fabs(k) < 1125899906842624.0);
