@@ -935,7 +935,9 @@ def rotate(x, positions, rotary: Rotary, out=None, transpose: bool = False, stre
     """sekv_rotate: x [n_tokens][heads][d] (tokens may be strided; float32 or bfloat16) turned by positions int32
     [n_tokens]; out may be x itself.  transpose: the other way, which is the gradient with respect to x.  Where x requires
     a gradient the result has one, of any order; out cannot be given then."""
-    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (x, out)):
+    if not isinstance(x, torch.Tensor) or x.dim() != 3 or x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("x: float32 or bfloat16 [n_tokens][heads][d]")
+    if torch.is_grad_enabled() and (x.requires_grad or isinstance(out, torch.Tensor) and out.requires_grad):
         if out is not None:
             raise ValueError("out: no gradient passes through a tensor that is given")
         with _on(x.device, stream, "rows")[0]:               # so that the backward pass runs on this stream, too
@@ -964,8 +966,6 @@ class _Rotate(torch.autograd.Function):
 
 
 def _rotate(x, positions, rotary, out, transpose, stream):
-    if not isinstance(x, torch.Tensor) or x.dim() != 3 or x.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("x: float32 or bfloat16 [n_tokens][heads][d]")
     _, heads, d = x.shape
     dev, dt = x.device, x.dtype
     n, xp, sx = _rows_of(dt, d, x, "x", heads, dev)
