@@ -3,8 +3,9 @@
 //
 // What bounds it: the matrix cores and the softmax's vector instructions together.  A wave takes 32
 // rows; per tile it issues 32 matrix instructions (32x32x16, half scores, half values), and 2048 scores
-// cost it about 4 vector instructions and one exponential each for 64 lanes, so the two units are about
-// equally busy and two workgroups share a compute unit to keep both fed.  Keys and values are fetched
+// cost it about 4 vector instructions and one exponential each for 64 lanes (177 in all over bfloat16 pages; 254 in
+// 4 bits, with the conversions and the order in which LDS is filled), so the two units are about equally busy and two
+// workgroups share a compute unit to keep both fed.  Keys and values are fetched
 // once per workgroup (each wave one block of 16 keys, which lies in one page), a tile ahead: bfloat16
 // straight into LDS, codes of 8 and 4 bits through registers, where they become scaled bfloat16, so that the rest
 // knows one type only.
@@ -121,7 +122,8 @@ struct Stage<E2M1, D> {
     }
     // Eight lanes, of two rows, write at a time, 16 bytes each, and the 128 bytes that they fill should not share banks.
     // So a lane takes its pieces in an order of its own: number u ^ turn in step u.  All in the order of u, with two lanes
-    // (keys) or four (values) in the same banks, 2048 tokens over 32768 take 1121 us instead of 1097.
+    // (keys) or four (values) in the same banks, 2048 tokens over 32768 take 1121 us instead of 1097.  The order costs
+    // 32 vector instructions a tile: the selections, and the places, which depend on the lane alone.
     __device__ static wv turned(wv x, int turn) {
         wv y;
 #pragma unroll

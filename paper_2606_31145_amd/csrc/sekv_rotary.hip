@@ -2,9 +2,10 @@
 //
 // A row is read once and written once, which is what bounds long calls: 32768 tokens of 32 heads of 128 in bfloat16
 // (537 MB) take 99 us (5.4 TB/s, a copy 5.1), those of four 8192-token chunks with 8 heads of keys and values into 4 bits
-// (707 MB) 138 us (5.1 TB/s).  Short ones are a chain of dependent reads: 32 tokens of 32 heads 3 us, with their keys 6.
+// (707 MB) 138 us (5.1 TB/s).  Short ones are a chain of dependent reads: 32 tokens of 32 heads 3 us, with their keys 6.1,
+// of which a wave spends most on looking up its tokens one after another.
 // The unit of work is a wave, so that nothing waits for a workgroup (workgroups of 16 tokens, one row a lane in flight: 132
-// and 185 us):
+// and 185 us, but 5.2 for the 32 tokens with their keys):
 //   - queries: one token and a range of its heads, which lie together.  A lane forms one pair's cos and sin, the wave
 //     meets in LDS, and each lane takes those of its piece for all the heads.
 //   - keys and values: as many consecutive tokens as a wave holds rows side by side, head by head, for consecutive tokens
